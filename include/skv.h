@@ -548,6 +548,63 @@ skv_status skv_unpack_groups(const skv_config* cfg, const skv_group_spec* spec, 
 skv_status skv_link(void* dst, const void* src, uint64_t bytes, void* host_staging,
                     hipStream_t stream);
 
+/* Attention beside the codec: over the prompts whose K and V it packs, and over
+ * the paged cache it fills.  For a query with visible keys t the result is
+ * out = sum_t softmax_t(scale q.k_t) v_t and lse = log sum_t exp(scale q.k_t)
+ * (natural logarithm); a query that sees no key gets out = 0 and lse =
+ * -infinity.  Query head hq reads KV head hq / (Hq / H).  Products are exact,
+ * sums binary32, probabilities rounded to the 16-bit type before their product
+ * with V, results rounded once.  NaN and infinities follow IEEE softmax over the
+ * visible keys; hidden keys' K and V, whatever they hold, have no effect.
+ * Results of a call are the same every time. */
+enum { SKV_DTYPE_F16 = 0, SKV_DTYPE_BF16 = 1 };
+
+/* What the requests of a prompt attention call share.  Strides are in elements,
+ * multiples of 8, positive; a row's d elements are contiguous.  Validity: dtype
+ * F16 or BF16; H >= 1, num_q_heads a multiple of H, at most 2^16; d in {32, 64,
+ * 128, 256}; scale positive and finite. */
+typedef struct skv_attn_config {
+  int32_t dtype;        /* SKV_DTYPE_* of q, k, v and out                         */
+  int32_t num_q_heads;  /* Hq                                                     */
+  int32_t num_kv_heads; /* H                                                      */
+  int32_t head_dim;     /* d                                                      */
+  int32_t causal;       /* 1: query i of a request sees keys j <= i + num_keys -
+                           num_queries; 0: every key                              */
+  float scale;          /* of the logits, usually 1 / sqrt(d)                     */
+  int64_t q_token_stride, q_head_stride;
+  int64_t out_token_stride, out_head_stride;
+} skv_attn_config;
+
+/* One sequence.  Device pointers, 16-byte aligned (lse: 4).  K and V share their
+ * strides (each below 2^25 for tokens): [H][n][d] as the codec packs, or packed
+ * by token with other sequences.  out may not overlap the inputs. */
+typedef struct skv_attn_request {
+  int32_t num_queries;  /* >= 0                                                   */
+  int32_t num_keys;     /* >= 0                                                   */
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  float* lse;           /* binary32 [num_queries][Hq], or NULL                     */
+  int64_t kv_token_stride, kv_head_stride;
+} skv_attn_request;
+
+/* Host only.  Workspace bytes with which skv_attn_prompt can split these
+ * requests' keys over the GPU (few queries over many keys); 0 where it would not.
+ * Pointers are not looked at. */
+skv_status skv_attn_prompt_workspace_size(const skv_attn_config* cfg, const skv_attn_request* reqs, int32_t count,
+                                          uint64_t* bytes);
+
+/* Attention of `count` sequences of any lengths (up to 48 per launch).  ws: NULL,
+ * or ws_bytes of device memory, 16-byte aligned; with at least
+ * skv_attn_prompt_workspace_size bytes, sequences with few queries and many keys
+ * run split over the GPU (results differ from the unsplit ones by rounding
+ * alone), with less they run unsplit.  Calls that share ws must be ordered on one
+ * stream.  Every request is checked before anything is enqueued.  Kernel
+ * launches only: the call can be captured in a HIP graph. */
+skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* reqs, int32_t count, void* ws,
+                           uint64_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

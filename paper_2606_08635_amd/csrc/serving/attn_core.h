@@ -1,0 +1,369 @@
+// What the attention kernels share: one wave's online softmax(Q K^T) V over
+// key tiles that its workgroup stages through shared memory.
+//
+// For a query q with visible keys t the kernels compute
+//   z_t = alpha q.k_t (alpha = scale log2 e),  m = max z_t,
+//   l = sum 2^(z_t - m),  o = (1/l) sum 2^(z_t - m) v_t,  lse = (m + log2 l) ln 2
+// in one pass over the keys.  Both products run on v_mfma_f32_32x32x16 with
+// binary32 accumulation.  The logits are formed transposed (keys as MFMA rows,
+// queries as columns), so a lane holds 16 keys of one query per 32-key tile,
+// keeps that query's m and l in registers, and its exponentials are already
+// the second product's B operand (o^T = V^T P^T): no value crosses lanes
+// between the two products.  V is read from its row-major stage by gfx950's
+// transposing LDS reads (ds_read_b64_tr_b16).
+//
+// Rows are packed: the G = Hq / H query heads that share a KV head are rows of
+// one product (row r is token r / G, head h G + r % G), so K and V of a head are
+// staged once for all of them, and one token per request still gives G rows.
+//
+// Roundings: products exact, sums, m, l and o in binary32; the probabilities are
+// rounded (nearest even) to the inputs' 16-bit type for the second product --
+// the MFMA takes both operands in one type -- while l sums them unrounded; the
+// result is rounded once to the output type.
+#pragma once
+
+#include "../device_util.h"
+
+namespace skv {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+struct TypeF16 {
+  typedef _Float16 elem;
+  typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kInf = 0x7C00u, kOne = 0x3C00u;
+  __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+struct TypeBF16 {
+  typedef __bf16 elem;
+  typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kInf = 0x7F80u, kOne = 0x3F80u;
+  __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+
+// Two binary32 values rounded (nearest even) to E and packed low | high.
+template <class E>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const floatx2 f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, typename E::vec2));
+}
+
+// Row of accumulator register r in lane-half hf of a 32x32 MFMA result (the
+// column is lane % 32).
+__device__ __forceinline__ int mfma_row(int r, int hf) { return 8 * (r >> 2) + 4 * hf + (r & 3); }
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const uint8_t*)p));
+}
+
+// Direct global-to-LDS load: lane i's 16 bytes at src land at LDS byte address
+// lds_base + 16 i.  From inline assembly, so that the compiler does not count it
+// among its own loads; the tile loop waits for it itself (wait_direct_loads).
+__device__ __forceinline__ void direct_load(const void* src, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds_base) : "memory", "m0");
+}
+__device__ __forceinline__ void direct_load(const void* uniform_base, uint32_t offset, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(uniform_base), "s"(lds_base)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void wait_direct_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Workgroup barrier that waits for this wave's shared-memory accesses but not
+// for its global loads in flight.
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Shared-memory stage of kKeys keys: K rows, then V rows, each row D 16-bit
+// values as kCpr chunks of 16 bytes, chunk c of row r at place c ^ swz(r).  The
+// swizzle makes two access patterns free of bank conflicts at once: the first
+// product reads one chunk of 16 consecutive rows (swz takes each value once over
+// the rows that share 256 bytes of banks), the second reads 64 consecutive bytes
+// of 4 consecutive rows (swz differs in the bits that select the 64-byte group).
+template <int D>
+struct Stage {
+  static constexpr int kWaves = 4;
+  static constexpr int kThreads = kWaves * 64;
+  static constexpr int kKeys = 64;
+  static constexpr int kCpr = D / 8;
+  static constexpr int kPitch = D * 2;
+  static constexpr int kHalf = kKeys * kPitch;  // bytes of K, and of V
+  static constexpr int kBytes = 2 * kHalf;
+  static constexpr int kPieces = kKeys * kCpr / kThreads;  // 16-byte loads of K per thread, and of V
+  static constexpr int kRowStep = kThreads / kCpr;         // rows between a thread's pieces
+  // waves per SIMD that the registers allow: o and Q alone are 3 D / 4 registers
+  static constexpr int kWavesPerSimd = D >= 256 ? 1 : 2;
+  static_assert(kKeys * kCpr % kThreads == 0, "whole pieces per thread");
+  __device__ static constexpr int swz(int r) {
+    return D >= 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : D == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
+  }
+};
+
+// One wave's 32 query rows: state and arithmetic.  NS: 32-key tiles that it
+// takes per step.
+template <class E, int D, int NS>
+struct WaveAttention {
+  typedef typename E::vec8 vec8;
+  typedef Stage<D> S;
+  static constexpr int kSteps = D / 16;  // MFMA steps of a logit
+  static constexpr int kTiles = D / 32;  // 32-channel tiles of o
+  // A step is exponentiated against the current reference m first, without its
+  // maximum; only where that gives a sum past kHigh (or a NaN: m still -inf) is
+  // the maximum taken, m raised and o rescaled.  2^15 keeps every probability
+  // inside binary16.  m is some earlier step's maximum, so what underflows
+  // against it is negligible beside what is in the sum already.
+  static constexpr float kHigh = 32768.0f;
+
+  vec8 q[kSteps];
+  floatx16 o[kTiles];
+  float m, l;
+  uint32_t kaddr[kSteps];               // LDS addresses in the first stage buffer
+  uint32_t vaddr[kTiles < 4 ? kTiles : 4][2];
+  uint32_t vrows;                       // this lane's 16 bytes of the wave's V rows
+
+  // first: the wave's first key of a stage
+  __device__ __forceinline__ void init(const void* stage, int first) {
+    const int lane = threadIdx.x & 63, hf = lane >> 5, j = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
+    const uint32_t base = lds_address(stage) + static_cast<uint32_t>(first * S::kPitch);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      kaddr[s] = base + static_cast<uint32_t>(j * S::kPitch + 16 * ((2 * s + hf) ^ S::swz(j)));
+      asm volatile("" : "+v"(kaddr[s]));  // one register each: tile offsets become immediates
+    }
+#pragma unroll
+    for (int dt = 0; dt < (kTiles < 4 ? kTiles : 4); ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int row = 8 * u + 4 * hf + (i >> 2);
+        const int chunk = 4 * dt + 2 * g + ((i & 3) >> 1);
+        vaddr[dt][u] =
+            base + static_cast<uint32_t>(S::kHalf + row * S::kPitch + 16 * (chunk ^ S::swz(row)) + 8 * (i & 1));
+        asm volatile("" : "+v"(vaddr[dt][u]));
+      }
+    vrows = base + static_cast<uint32_t>(S::kHalf + 16 * lane);
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) o[dt] = floatx16{};
+    m = -INFINITY;
+    l = 0.0f;
+  }
+
+  __device__ __forceinline__ void load_q(const void* row) {
+    const uint8_t* p = static_cast<const uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4*>(p + 32 * s));
+  }
+
+  __device__ static __forceinline__ u32x4 lds16(uint32_t addr) {
+    typedef __attribute__((address_space(3))) const u32x4* ptr;
+    return *reinterpret_cast<ptr>(static_cast<uintptr_t>(addr));
+  }
+  // channels 32 dt + lane % 32 of the 8 keys 16 s + {4 hf .. + 3, 8 + 4 hf .. + 3}
+  template <int OFF>
+  __device__ __forceinline__ u32x4 v_operand(int dt, int s) const {
+    typedef __attribute__((address_space(3))) shortx4* ptr;
+    u32x4 a;
+    const uint32_t off = static_cast<uint32_t>(OFF + 16 * s * S::kPitch + (dt >> 2) * 256);
+    const u32x2 lo = __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ptr>(static_cast<uintptr_t>(vaddr[dt & 3][0] + off))));
+    const u32x2 hi = __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ptr>(static_cast<uintptr_t>(vaddr[dt & 3][1] + off))));
+    a.x = lo.x;
+    a.y = lo.y;
+    a.z = hi.x;
+    a.w = hi.y;
+    return a;
+  }
+
+  __device__ __forceinline__ void rescale(float f) {
+    l *= f;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dt][r] *= f;
+  }
+
+  // Whether V holds an infinity or NaN in the wave's keys of this stage.
+  template <int OFF>
+  __device__ __forceinline__ bool v_not_finite() const {
+    uint32_t top = 0;
+#pragma unroll
+    for (int u = 0; u < NS * 32 * S::kPitch / 1024; ++u)
+      top = max(top, absmax_bits8(lds16(vrows + static_cast<uint32_t>(OFF + 1024 * u))));
+    return __any(top >= E::kInf);
+  }
+
+  // o += V^T P^T for keys with p != 0 alone: V's infinities and NaN are taken out
+  // of the product and counted in products of their own, so that one that is
+  // hidden from a row (p = 0) does not reach it.
+  template <int OFF>
+  __device__ __forceinline__ void accumulate_safe(const u32x4 (&p)[2 * NS]) {
+    auto each = [](u32x4 x, auto f) {
+      u32x4 y;
+      y.x = f(x.x & 0xFFFFu) | f(x.x >> 16) << 16;
+      y.y = f(x.y & 0xFFFFu) | f(x.y >> 16) << 16;
+      y.z = f(x.z & 0xFFFFu) | f(x.z >> 16) << 16;
+      y.w = f(x.w & 0xFFFFu) | f(x.w >> 16) << 16;
+      return y;
+    };
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) {
+      floatx16 pos{}, neg{};
+#pragma unroll
+      for (int s = 0; s < 2 * NS; ++s) {
+        const u32x4 a = v_operand<OFF>(dt, s);
+        const u32x4 seen = each(p[s], [](uint32_t w) { return (w & 0x7FFFu) ? E::kOne : 0u; });
+        const u32x4 fin = each(a, [](uint32_t w) { return (w & 0x7FFFu) >= E::kInf ? 0u : w; });
+        const u32x4 up = each(a, [](uint32_t w) { return (w & 0x7FFFu) >= E::kInf && w != (E::kInf | 0x8000u) ? E::kOne : 0u; });
+        const u32x4 down = each(a, [](uint32_t w) { return (w & 0x7FFFu) >= E::kInf && w != E::kInf ? E::kOne : 0u; });
+        o[dt] = E::mfma(__builtin_bit_cast(vec8, fin), __builtin_bit_cast(vec8, p[s]), o[dt]);
+        pos = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), pos);
+        neg = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), neg);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (pos[r] > 0.0f) o[dt][r] += INFINITY;
+        if (neg[r] > 0.0f) o[dt][r] -= INFINITY;
+      }
+    }
+  }
+
+  // One step: the wave's NS * 32 keys of the stage at byte offset OFF of the
+  // stage area.  visible(n, r): whether key mfma_row(r, hf) of tile n is seen by
+  // the lane's query; asked only where MASK.
+  template <int OFF, bool MASK, class Visible>
+  __device__ __forceinline__ void step(float alpha, Visible visible) {
+    floatx16 x[NS];
+#pragma unroll
+    for (int n = 0; n < NS; ++n) x[n] = floatx16{};
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+        x[n] = E::mfma(__builtin_bit_cast(vec8, lds16(kaddr[s] + static_cast<uint32_t>(OFF + n * 32 * S::kPitch))), q[s], x[n]);
+    float e[NS][16];
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (MASK && !visible(n, r)) x[n][r] = -INFINITY;
+        e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -m));
+      }
+      float t[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) t[r] = e[n][r] + e[n][r + 8];
+      sum += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    }
+    if (__any(!(sum <= kHigh))) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
+      const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, top * alpha));
+      const float mn = fmaxf(m, fmaxf(__builtin_bit_cast(float, p.lo), __builtin_bit_cast(float, p.hi)));
+      const float ref = mn == -INFINITY ? 0.0f : mn;  // nothing seen yet: every probability 0
+      rescale(__builtin_amdgcn_exp2f(m - ref));
+      m = mn;
+      sum = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -ref));
+          sum += e[n][r];
+        }
+    }
+    l += sum;
+    u32x4 p[2 * NS];
+#pragma unroll
+    for (int s = 0; s < 2 * NS; ++s) {
+      const float* f = &e[s >> 1][8 * (s & 1)];
+      p[s].x = pack2<E>(f[0], f[1]);
+      p[s].y = pack2<E>(f[2], f[3]);
+      p[s].z = pack2<E>(f[4], f[5]);
+      p[s].w = pack2<E>(f[6], f[7]);
+    }
+    if constexpr (MASK) {
+      if (v_not_finite<OFF>()) {
+        accumulate_safe<OFF>(p);
+        return;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < 2 * NS; ++s)
+#pragma unroll
+      for (int dt = 0; dt < kTiles; ++dt)
+        o[dt] = E::mfma(__builtin_bit_cast(vec8, v_operand<OFF>(dt, s)), __builtin_bit_cast(vec8, p[s]), o[dt]);
+  }
+  // Adds the state that another wave left at `from` (write_state) to this one's.
+  static constexpr int kStateBytes = (D / 2 + 2) * 256;  // per wave
+  __device__ __forceinline__ void write_state(uint8_t* to) const {
+    float* f = reinterpret_cast<float*>(to) + (threadIdx.x & 63);
+    f[0] = m;
+    f[64] = l;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) f[64 * (2 + 16 * dt + r)] = o[dt][r];
+  }
+  __device__ __forceinline__ void merge_state(const uint8_t* from) {
+    const float* f = reinterpret_cast<const float*>(from) + (threadIdx.x & 63);
+    const float m2 = f[0], mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.0f : mn;
+    const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(m2 - ref);
+    m = mn;
+    l = l * a + f[64] * b;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dt][r] = o[dt][r] * a + f[64 * (2 + 16 * dt + r)] * b;
+  }
+  // l over both lane-halves.
+  __device__ __forceinline__ float total() const {
+    const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, l));
+    return __builtin_bit_cast(float, p.lo) + __builtin_bit_cast(float, p.hi);
+  }
+  // The row's result, rounded to E: a lane-half writes 16 contiguous bytes.
+  __device__ __forceinline__ void write_out(void* row, float inv) const {
+    uint8_t* p = static_cast<uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = pack2<E>(o[dt][8 * h + 2 * i] * inv, o[dt][8 * h + 2 * i + 1] * inv);
+        // the halves hold channels 4 hf .. + 3 of two groups of 8: each half takes one group
+        const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        *reinterpret_cast<u32x4*>(p + 64 * dt + 32 * h) = u32x4{s0[0], s1[0], s0[1], s1[1]};
+      }
+  }
+  // The row's unnormalized sum in binary32.
+  __device__ __forceinline__ void write_partial(float* row) const {
+    float* p = row + 4 * ((threadIdx.x >> 5) & 1);
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+#pragma unroll
+      for (int h = 0; h < 4; ++h)
+        *reinterpret_cast<floatx4*>(p + 32 * dt + 8 * h) =
+            floatx4{o[dt][4 * h], o[dt][4 * h + 1], o[dt][4 * h + 2], o[dt][4 * h + 3]};
+  }
+};
+
+__device__ __forceinline__ float inverse_or_zero(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+}  // namespace skv

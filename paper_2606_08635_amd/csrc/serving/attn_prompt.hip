@@ -1,0 +1,178 @@
+// Attention over whole prompts: packed sequences, grouped heads, causal or not.
+//
+// A workgroup owns up to 128 packed rows (attn_core.h) of one (request, KV head)
+// and walks the keys that any of them sees in tiles of 64, staged through two
+// shared-memory buffers by direct global-to-LDS loads: the next tile is in
+// flight while the current one is multiplied, and one barrier per tile orders
+// both.  Tiles past a wave's last visible key are skipped, and only tiles that a
+// row's limit cuts compare indexes.
+//
+// Order of the workgroups: KV heads fastest, so that consecutive workgroups --
+// which the hardware deals to the 8 XCDs in turn -- read different heads and an
+// XCD's L2 holds few of them; then the row blocks from the last to the first,
+// since the last ones see the most keys and the launch ends with short ones.
+#include "attn_core.h"
+#include "serving_internal.h"
+
+namespace skv {
+namespace {
+
+template <class E, int D, int KS>
+__global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void attn_prompt(const PromptArgs a) {
+  typedef Stage<D> S;
+  typedef WaveAttention<E, D, 2 / KS> Wave;
+  __shared__ __align__(1024) uint8_t stage[2 * S::kBytes];
+  const uint32_t block = blockIdx.x;
+  int ri = 0;
+  for (int step = 32; step > 0; step >>= 1)  // the last request that begins at or before this workgroup
+    if (ri + step < a.count && a.r[ri + step].begin <= block) ri += step;
+  const PromptDesc& r = a.r[ri];
+  const int rows = r.nq * a.G, per = a.row_tiles * 32;
+  const int nblk = (rows + per - 1) / per;
+  uint32_t at = block - r.begin;
+  const int h = static_cast<int>(at % static_cast<uint32_t>(a.H));
+  at /= static_cast<uint32_t>(a.H);
+  const int blk = nblk - 1 - static_cast<int>(at / static_cast<uint32_t>(r.splits));
+  const int split = static_cast<int>(at % static_cast<uint32_t>(r.splits));
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
+  const int rt = wave % a.row_tiles, ks = wave / a.row_tiles;
+  const int row0 = blk * per + rt * 32;  // the wave's first row
+  const bool active = ks < KS && row0 < rows;
+  const int row = min(row0 + (lane & 31), rows - 1);
+  const int token = row / a.G, head = h * a.G + row % a.G;
+  const int more = r.nk - r.nq;
+  const int limit = a.causal ? token + more : r.nk - 1;  // the row's last visible key
+  const int wave_min = __builtin_amdgcn_readfirstlane(limit);
+  const int wave_max = a.causal ? min(row0 + 31, rows - 1) / a.G + more : r.nk - 1;
+  const int block_max = a.causal ? min(blk * per + per - 1, rows - 1) / a.G + more : r.nk - 1;
+  const int all = block_max < 0 ? 0 : block_max / S::kKeys + 1;  // tiles that some row sees
+  const int t0 = static_cast<int>(static_cast<int64_t>(all) * split / r.splits);
+  const int t1 = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / r.splits);
+
+  Wave w;
+  w.init(stage, ks * 32);
+  w.load_q(r.q + token * a.q_token + head * a.q_head);
+
+  // this thread's pieces of a stage: row tid / kCpr + u * kRowStep, place tid % kCpr
+  const int prow = static_cast<int>(threadIdx.x) / S::kCpr, place = static_cast<int>(threadIdx.x) % S::kCpr;
+  const uint16_t* kbase = r.k + h * r.kv_head;
+  const uint16_t* vbase = r.v + h * r.kv_head;
+  const uint32_t token_bytes = static_cast<uint32_t>(r.kv_token * 2);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(stage) + static_cast<uint32_t>(wave * 1024));
+  auto issue = [&](int t, int buffer) {
+    const int64_t first = static_cast<int64_t>(t) * S::kKeys * r.kv_token;
+    const int last = r.nk - 1 - t * S::kKeys;  // rows past it repeat the last key: hidden from every row
+#pragma unroll
+    for (int u = 0; u < S::kPieces; ++u) {
+      const int rr = prow + u * S::kRowStep;
+      const uint32_t off = static_cast<uint32_t>(min(rr, last)) * token_bytes +
+                           16u * static_cast<uint32_t>(place ^ S::swz(rr));
+      const uint32_t to = lds0 + static_cast<uint32_t>(buffer * S::kBytes + u * S::kThreads * 16);
+      direct_load(kbase + first, off, to);
+      direct_load(vbase + first, off, to + S::kHalf);
+    }
+  };
+  auto tile = [&](int t, auto buffer) {
+    constexpr int OFF = decltype(buffer)::value * S::kBytes;
+    const int key0 = t * S::kKeys + ks * 32;
+    if (!active || key0 > wave_max) return;
+    const int mine = limit - key0 - 4 * hf;  // visible: 32 n + 8 (r / 4) + r % 4 <= mine
+    auto visible = [&](int n, int rr) { return 32 * n + 8 * (rr >> 2) + (rr & 3) <= mine; };
+    if (key0 + 64 / KS - 1 > wave_min) w.template step<OFF, true>(a.alpha, visible);
+    else w.template step<OFF, false>(a.alpha, visible);
+  };
+  if (t0 < t1) issue(t0, 0);
+  for (int t = t0; t < t1; t += 2) {
+    wait_direct_loads();
+    stage_barrier();
+    if (t + 1 < t1) issue(t + 1, 1);
+    tile(t, std::integral_constant<int, 0>{});
+    if (t + 1 >= t1) break;
+    wait_direct_loads();
+    stage_barrier();
+    if (t + 2 < t1) issue(t + 2, 0);
+    tile(t + 1, std::integral_constant<int, 1>{});
+  }
+  if constexpr (KS > 1) {  // the waves that took the other keys of the same rows
+    stage_barrier();
+    if (ks == 1) w.write_state(stage + rt * Wave::kStateBytes);
+    stage_barrier();
+    if (ks != 0) return;
+    w.merge_state(stage + rt * Wave::kStateBytes);
+  }
+  if (!active || row0 + (lane & 31) >= rows) return;  // (both lane-halves of a row stay: total and write_out pair them)
+  const float l = w.total();
+  if (r.splits > 1) {
+    const int64_t prow_at = r.rows_at + (static_cast<int64_t>(split) * a.H + h) * rows + row;
+    w.write_partial(a.part_o + prow_at * D);
+    if (hf == 0) *reinterpret_cast<floatx2*>(a.part_ml + 2 * prow_at) = floatx2{w.m, l};
+    return;
+  }
+  w.write_out(r.out + token * a.out_token + head * a.out_head, inverse_or_zero(l));
+  if (r.lse != nullptr && hf == 0) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, l);
+}
+
+// Joins the parts of requests with splits > 1: one wave per row.
+template <class E, int D>
+__global__ __launch_bounds__(256) void attn_prompt_join(const PromptArgs a, int ri) {
+  const PromptDesc& r = a.r[ri];
+  const int rows = r.nq * a.G;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // h * rows + row
+  if (at >= static_cast<int64_t>(rows) * a.H) return;
+  const int lane = threadIdx.x & 63;
+  const int h = static_cast<int>(at / rows), row = static_cast<int>(at % rows);
+  const int64_t stride = static_cast<int64_t>(rows) * a.H;
+  float m = -INFINITY;
+  for (int s = 0; s < r.splits; ++s) m = fmaxf(m, a.part_ml[2 * (r.rows_at + s * stride + at)]);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  constexpr int N = D >= 64 ? D / 64 : 1;
+  float l = 0.0f, o[N] = {};
+  for (int s = 0; s < r.splits; ++s) {
+    const int64_t p = r.rows_at + s * stride + at;
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - ref);
+    l += a.part_ml[2 * p + 1] * f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (D >= 64 || lane < D) o[i] += a.part_o[p * D + N * lane + i] * f;
+  }
+  const int token = row / a.G, head = h * a.G + row % a.G;
+  typename E::elem* out = reinterpret_cast<typename E::elem*>(r.out + token * a.out_token + head * a.out_head);
+  const float inv = inverse_or_zero(l);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (D >= 64 || lane < D) out[N * lane + i] = static_cast<typename E::elem>(o[i] * inv);
+  if (r.lse != nullptr && lane == 0) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(m, l);
+}
+
+template <class E, int D>
+hipError_t launch(const PromptArgs& a, hipStream_t stream) {
+  if (a.key_streams == 1) attn_prompt<E, D, 1><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
+  else attn_prompt<E, D, 2><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
+  hipError_t e = hipGetLastError();
+  for (int i = 0; i < a.count && e == hipSuccess; ++i) {
+    if (a.r[i].splits <= 1) continue;
+    const uint64_t rows = static_cast<uint64_t>(a.r[i].nq) * a.G * a.H;
+    attn_prompt_join<E, D><<<static_cast<uint32_t>((rows + 3) / 4), 256, 0, stream>>>(a, i);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+template <class E>
+hipError_t launch_d(const PromptArgs& a, int32_t d, hipStream_t stream) {
+  switch (d) {
+    case 32: return launch<E, 32>(a, stream);
+    case 64: return launch<E, 64>(a, stream);
+    case 128: return launch<E, 128>(a, stream);
+    default: return launch<E, 256>(a, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attn_prompt(const PromptArgs& a, int32_t dtype, int32_t d, hipStream_t stream) {
+  return dtype == SKV_DTYPE_F16 ? launch_d<TypeF16>(a, d, stream) : launch_d<TypeBF16>(a, d, stream);
+}
+
+}  // namespace skv

@@ -30,7 +30,8 @@ EXPORTED = ("skv_abi_version", "skv_status_string", "skv_plan_tiers", "skv_paylo
             "skv_pack_upgrade", "skv_unpack_upgrade", "skv_group_count", "skv_plan_groups",
             "skv_grouped_payload_size", "skv_group_workspace_size", "skv_prepare_groups", "skv_score_groups",
             "skv_assign_groups", "skv_pack_groups", "skv_unpack_groups", "skv_batch_workspace_size",
-            "skv_score_batch", "skv_assign_batch")
+            "skv_score_batch", "skv_assign_batch", "skv_attn_prompt_workspace_size", "skv_attn_prompt")
+DTYPE_F16, DTYPE_BF16 = 0, 1
 
 
 class SkvError(RuntimeError):
@@ -64,6 +65,19 @@ class ScoreRequest(ctypes.Structure):
 class GroupSpec(ctypes.Structure):
     _fields_ = [("granularity", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("budgets", ctypes.POINTER(ctypes.c_float))]
+
+
+class AttnConfig(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
+
+
+class AttnRequest(ctypes.Structure):
+    _fields_ = [("num_queries", ctypes.c_int32), ("num_keys", ctypes.c_int32), ("q", ctypes.c_void_p),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("kv_token_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64)]
 
 
 class Plan(ctypes.Structure):
@@ -116,6 +130,8 @@ def lib():
             "skv_batch_workspace_size": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, P(u64)]),
             "skv_score_batch": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, vp, vp]),
             "skv_assign_batch": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, vp, vp]),
+            "skv_attn_prompt_workspace_size": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, P(u64)]),
+            "skv_attn_prompt": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, vp, u64, vp]),
         }
         for name, (res, args) in sigs.items():
             fn = getattr(L, name)
@@ -498,6 +514,109 @@ def unpack_batch(cfg: Config, payloads, token_counts, block_tables, k_cache: tor
                                   _dev(k_cache, torch.float16, k_cache.numel(), "k_cache"),
                                   _dev(v_cache, torch.float16, v_cache.numel(), "v_cache"), nb, block_size,
                                   layer_begin, lc, _stream(stream)), "skv_unpack_batch")
+
+
+_ATTN_TYPES = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
+
+
+def _rows(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str) -> int:
+    """Device pointer of a tensor of `like`'s dtype and device and the given shape (None: any size), its last axis contiguous."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if not t.is_cuda or t.device != like.device:
+        raise ValueError(f"{name} must be a device tensor on q's device")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.numel() and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    return t.data_ptr()
+
+
+def _stride(t: torch.Tensor, axis: int) -> int:
+    """Stride of an axis; of one of a single place (torch gives any number there) the one that packing would give."""
+    return t.stride(axis) if t.shape[axis] > 1 else t.shape[-1]
+
+
+def attn_prompt_workspace_size(q_lens, kv_lens, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                               causal: bool = True) -> int:
+    """Workspace bytes with which attn_prompt splits these sequences' keys over the GPU (0: it would not)."""
+    count = len(q_lens)
+    if len(kv_lens) != count:
+        raise ValueError("q_lens and kv_lens differ in length")
+    cfg = AttnConfig(DTYPE_F16, num_q_heads, num_kv_heads, head_dim, int(causal), 1.0, 0, 0, 0, 0)
+    reqs = (AttnRequest * count)()
+    for r, nq, nk in zip(reqs, q_lens, kv_lens):
+        r.num_queries, r.num_keys = nq, nk
+    out = ctypes.c_uint64()
+    _check(lib().skv_attn_prompt_workspace_size(ctypes.byref(cfg), reqs, count, ctypes.byref(out)),
+           "skv_attn_prompt_workspace_size")
+    return out.value
+
+
+def attn_prompt(q: torch.Tensor, k, v, out: torch.Tensor, q_lens=None, kv_lens=None, causal: bool = True,
+                scale: Optional[float] = None, lse: Optional[torch.Tensor] = None,
+                ws: Optional[torch.Tensor] = None, stream=None):
+    """Attention of packed sequences: q and out [sum(q_lens)][Hq][d] (float16
+    or bfloat16, any token and head strides), sequence after sequence.  k, v:
+    packed the same way, [sum(kv_lens)][H][d], or a list with each sequence's
+    [H][n][d] (a layer of the codec's K and V).  q_lens defaults to one
+    sequence, kv_lens to q_lens (packed) or the lists' lengths; causal query i
+    sees keys j <= i + n_keys - n_queries.  scale defaults to 1/sqrt(d).  lse:
+    float32 [sum(q_lens)][Hq], written when given.  ws:
+    attn_prompt_workspace_size bytes, or None (no splitting of the keys)."""
+    if q.dtype not in _ATTN_TYPES:
+        raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens][heads][d]")
+    total, Hq, d = q.shape
+    lists = isinstance(k, (list, tuple))
+    if lists != isinstance(v, (list, tuple)) or (lists and len(k) != len(v)):
+        raise ValueError("k and v must both be packed tensors or lists of one length")
+    q_lens = [total] if q_lens is None else [int(n) for n in q_lens]
+    count = len(q_lens)
+    if kv_lens is None:
+        kv_lens = [x.shape[1] for x in k] if lists else q_lens
+    kv_lens = [int(n) for n in kv_lens]
+    if len(kv_lens) != count or (lists and len(k) != count):
+        raise ValueError("q_lens, kv_lens and the lists of k and v differ in length")
+    if min(q_lens, default=0) < 0 or min(kv_lens, default=0) < 0 or sum(q_lens) != total:
+        raise ValueError("q_lens must be non-negative and add up to q's tokens")
+    qp, op = _rows(q, q, q.shape, "q"), _rows(out, q, q.shape, "out")
+    lp = None if lse is None else _dev(lse, torch.float32, total * Hq, "lse")
+    H = (k[0].shape[0] if count else 1) if lists else k.shape[1]
+    cfg = AttnConfig(_ATTN_TYPES[q.dtype], Hq, H, d, int(causal), d ** -0.5 if scale is None else scale,
+                     _stride(q, 0), _stride(q, 1), _stride(out, 0), _stride(out, 1))
+    if not lists:
+        if sum(kv_lens) != k.shape[0]:
+            raise ValueError("kv_lens must add up to k's tokens")
+        kp, vp = _rows(k, q, (sum(kv_lens), H, d), "k"), _rows(v, q, k.shape, "v")
+        ks, hs = _stride(k, 0), _stride(k, 1)
+        if (_stride(v, 0), _stride(v, 1)) != (ks, hs):
+            raise ValueError("k and v must have the same strides")
+    reqs = (AttnRequest * count)()
+    qo = oo = lo = ko = 0
+    for i in range(count):
+        r, nq, nk = reqs[i], q_lens[i], kv_lens[i]
+        r.num_queries, r.num_keys = nq, nk
+        r.q, r.out = qp + qo, op + oo
+        if lp is not None:
+            r.lse = lp + lo
+        if lists:
+            r.k, r.v = _rows(k[i], q, (H, nk, d), "k"), _rows(v[i], q, (H, nk, d), "v")
+            r.kv_token_stride, r.kv_head_stride = _stride(k[i], 1), _stride(k[i], 0)
+            if nk and (_stride(v[i], 1), _stride(v[i], 0)) != (r.kv_token_stride, r.kv_head_stride):
+                raise ValueError("k and v must have the same strides")
+        else:
+            r.k, r.v, r.kv_token_stride, r.kv_head_stride = kp + ko, vp + ko, ks, hs
+            ko += 2 * ks * nk
+        qo += 2 * cfg.q_token_stride * nq
+        oo += 2 * cfg.out_token_stride * nq
+        lo += 4 * Hq * nq
+    wsp = None if ws is None or ws.numel() == 0 else _dev(ws, torch.uint8, 0, "ws")
+    _check(lib().skv_attn_prompt(ctypes.byref(cfg), reqs, count, wsp, 0 if wsp is None else ws.numel(),
+                                 _stream(stream)), "skv_attn_prompt")
 
 
 def link(dst: torch.Tensor, src: torch.Tensor, nbytes: int, host_staging: Optional[torch.Tensor] = None,
