@@ -605,6 +605,56 @@ skv_status skv_attn_prompt_workspace_size(const skv_attn_config* cfg, const skv_
 skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* reqs, int32_t count, void* ws,
                            uint64_t ws_bytes, hipStream_t stream);
 
+/* Attention of the newest tokens of B requests over one layer of a paged cache
+ * ([num_blocks][block_size][H][d], one layer of what skv_unpack fills). */
+typedef struct skv_decode_config {
+  int32_t dtype;         /* SKV_DTYPE_* of q, the cache and out                   */
+  int32_t num_requests;  /* B                                                     */
+  int32_t num_queries;   /* Lq: newest tokens of each request, already in the
+                            cache (1; more to verify drafted tokens)              */
+  int32_t num_q_heads, num_kv_heads, head_dim; /* as skv_attn_config              */
+  int32_t num_blocks, block_size;              /* num_blocks * block_size < 2^31  */
+  int32_t table_width;   /* entries of a request's block table                    */
+  int32_t max_len;       /* about the longest request's tokens: sizes the launch;
+                            any request may be shorter or longer                  */
+  int32_t prefix_len;    /* tokens at the start of every request that are the same
+                            cache rows: a multiple of block_size whose entries in
+                            every request's table are those of request 0, with the
+                            same tiers; 0 where nothing is shared                 */
+  int32_t tier_len;      /* tokens that the tier maps cover (later ones are kept) */
+  float scale;
+  int64_t q_request_stride, q_token_stride, q_head_stride; /* elements, multiples of 8 */
+  int64_t out_request_stride, out_token_stride, out_head_stride;
+  int64_t table_stride;  /* entries between requests' tables, >= table_width      */
+  int64_t tier_request_stride, tier_head_stride; /* bytes between requests' and KV
+                            heads' tier maps (0: one map for all)                 */
+} skv_decode_config;
+
+/* Host only.  Device workspace bytes of skv_attn_decode: the partial results of
+ * the parts that cfg's work is cut into.  Looks at the counts, lengths and
+ * dimensions of cfg alone (and not at dtype, scale, strides or the cache). */
+skv_status skv_attn_decode_workspace_size(const skv_decode_config* cfg, uint64_t* bytes);
+
+/* q: [B][Lq][Hq][d] by cfg's strides; k_cache, v_cache: the layer; tables:
+ * int32 [B][table_stride]; lens: int32[B], tokens of each request in the cache, its
+ * Lq newest among them.  Query i of request b sees position t when t <= lens[b] -
+ * Lq + i and its tier is not SKV_TIER_DROP (tiers: uint8, NULL: all kept) -- the
+ * mask that a consumer of skv_unpack's output has to apply.  Positions below
+ * prefix_len are read through request 0's table and tiers, once for the batch; a
+ * request that ends inside the prefix sees its own tokens of it.  lens and tables
+ * are read on the device, so a captured call follows them.  out: [B][Lq][Hq][d];
+ * lse: binary32 [B][Lq][Hq], or NULL.  dev_status (may be NULL): set to
+ * SKV_ERR_FORMAT where a table entry in use is outside [0, num_blocks) (its
+ * tokens are left out) or a length outside [0, table_width * block_size] (taken to
+ * the nearer end); never cleared, so one check serves many steps.  ws:
+ * skv_attn_decode_workspace_size bytes (ws_bytes; SKV_ERR_CAPACITY if less), may
+ * be NULL where that is 0.  Calls that share ws must be ordered on one stream.
+ * Alignment 16 (tables, lens, lse, dev_status 4, tiers any).  Kernel launches
+ * only: the call can be captured in a HIP graph. */
+skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const void* k_cache, const void* v_cache,
+                           const int32_t* tables, const int32_t* lens, const uint8_t* tiers, void* out, float* lse,
+                           uint32_t* dev_status, void* ws, uint64_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -366,4 +366,54 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// Joins the parts of one row: part s is row first + s * stride of the partial
+// results.  A wave takes a row, its lanes D / 64 channels each (at D = 32 the
+// lower half, and lanes past D are given nothing to write).
+template <int D>
+struct JoinedRow {
+  static constexpr int kPer = D >= 64 ? D / 64 : 1;
+  typedef float vec __attribute__((ext_vector_type(kPer)));
+  float m = -INFINITY, l = 0.0f, o[kPer] = {};
+
+  __device__ __forceinline__ JoinedRow(const float* part_o, const float* part_ml, int64_t first, int64_t stride,
+                                       int parts) {
+    const int lane = threadIdx.x & 63;
+    const float* po = part_o + kPer * (D >= 64 ? lane : lane & 31);
+    for (int s0 = 0; s0 < parts; s0 += 64) {  // references and sums of up to 64 parts at once
+      floatx2 ml = {-INFINITY, 0.0f};
+      if (s0 + lane < parts) ml = *reinterpret_cast<const floatx2*>(part_ml + 2 * (first + (s0 + lane) * stride));
+      float top = ml.x;
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+      const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
+      const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+      float sum = ml.y * f;  // 0 of a part that saw nothing
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+      l = l * keep + sum;
+      m = mn;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) o[i] *= keep;
+      const uint64_t seen = __ballot(ml.x != -INFINITY || ml.y != 0.0f);  // the others wrote no sums
+      const int n = min(64, parts - s0);
+#pragma unroll 4
+      for (int s = 0; s < n; ++s) {
+        const float fs = __shfl(f, s);
+        if (!(seen >> s & 1)) continue;
+        const vec x = *reinterpret_cast<const vec*>(po + (first + (s0 + s) * stride) * D);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] += x[i] * fs;
+      }
+    }
+  }
+  template <class E>
+  __device__ __forceinline__ void write(typename E::elem* out) const {
+    const int lane = threadIdx.x & 63;
+    const float inv = inverse_or_zero(l);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (D >= 64 || lane < D) out[kPer * lane + i] = static_cast<typename E::elem>(o[i] * inv);
+  }
+};
+
 }  // namespace skv

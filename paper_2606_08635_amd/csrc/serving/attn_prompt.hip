@@ -122,27 +122,10 @@ __global__ __launch_bounds__(256) void attn_prompt_join(const PromptArgs a, int 
   if (at >= static_cast<int64_t>(rows) * a.H) return;
   const int lane = threadIdx.x & 63;
   const int h = static_cast<int>(at / rows), row = static_cast<int>(at % rows);
-  const int64_t stride = static_cast<int64_t>(rows) * a.H;
-  float m = -INFINITY;
-  for (int s = 0; s < r.splits; ++s) m = fmaxf(m, a.part_ml[2 * (r.rows_at + s * stride + at)]);
-  const float ref = m == -INFINITY ? 0.0f : m;
-  constexpr int N = D >= 64 ? D / 64 : 1;
-  float l = 0.0f, o[N] = {};
-  for (int s = 0; s < r.splits; ++s) {
-    const int64_t p = r.rows_at + s * stride + at;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * p] - ref);
-    l += a.part_ml[2 * p + 1] * f;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (D >= 64 || lane < D) o[i] += a.part_o[p * D + N * lane + i] * f;
-  }
+  const JoinedRow<D> j(a.part_o, a.part_ml, r.rows_at + at, static_cast<int64_t>(rows) * a.H, r.splits);
   const int token = row / a.G, head = h * a.G + row % a.G;
-  typename E::elem* out = reinterpret_cast<typename E::elem*>(r.out + token * a.out_token + head * a.out_head);
-  const float inv = inverse_or_zero(l);
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (D >= 64 || lane < D) out[N * lane + i] = static_cast<typename E::elem>(o[i] * inv);
-  if (r.lse != nullptr && lane == 0) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(m, l);
+  j.template write<E>(reinterpret_cast<typename E::elem*>(r.out + token * a.out_token + head * a.out_head));
+  if (r.lse != nullptr && lane == 0) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(j.m, j.l);
 }
 
 template <class E, int D>

@@ -107,6 +107,49 @@ skv_status prompt_launches(const skv_attn_config* c, const skv_attn_request* req
   return SKV_OK;
 }
 
+// How skv_attn_decode cuts its work (the counts, lengths and dimensions of c are
+// valid).
+struct DecodePlan {
+  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, tail_parts, tail_blocks, tail_tiles;
+  uint64_t prefix_groups, groups, part_bytes;
+};
+
+int32_t row_tiles(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
+DecodePlan plan_decode(const skv_decode_config* c) {
+  DecodePlan p{};
+  const int64_t H = c->num_kv_heads, G = c->num_q_heads / H, own = c->num_queries * G, all = own * c->num_requests;
+  const int64_t tail = std::max(0, c->max_len - c->prefix_len);
+  const int64_t want = 2 * kCus;
+  auto up = [](int64_t x, int64_t to) { return (x + to - 1) / to; };
+  p.tail_tiles = row_tiles(own);
+  p.tail_blocks = static_cast<int32_t>(up(own, 32 * p.tail_tiles));
+  const int64_t tails = c->num_requests * H * p.tail_blocks;
+  p.tail_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({up(want, tails), up(tail, 128), 256})));
+  if (c->prefix_len > 0) {
+    p.prefix_tiles = row_tiles(all);
+    p.prefix_blocks = static_cast<int32_t>(up(all, 32 * p.prefix_tiles));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({up(want, H * p.prefix_blocks), up(c->prefix_len, 128), 256}));
+    p.prefix_chunk = static_cast<int32_t>(up(up(c->prefix_len, parts), 64) * 64);
+    p.prefix_parts = static_cast<int32_t>(up(c->prefix_len, p.prefix_chunk));
+    p.prefix_groups = static_cast<uint64_t>(H * p.prefix_blocks * p.prefix_parts);
+  }
+  p.groups = p.prefix_groups + static_cast<uint64_t>(tails * p.tail_parts);
+  const int64_t parts = p.prefix_parts + p.tail_parts;
+  if (parts > 1) p.part_bytes = static_cast<uint64_t>(parts * H * all) * static_cast<uint64_t>(c->head_dim + 2) * 4u;
+  return p;
+}
+
+skv_status check_decode_sizes(const skv_decode_config* c) {
+  if (c == nullptr || !shape_ok(SKV_DTYPE_F16, c->num_q_heads, c->num_kv_heads, c->head_dim, 1.0f))
+    return SKV_ERR_INVALID_ARG;
+  if (c->num_requests < 0 || c->num_queries < 1 || c->max_len < 0 || c->prefix_len < 0) return SKV_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(c->num_requests) * c->num_queries > (1 << 20) ||
+      static_cast<int64_t>(c->num_requests) * c->num_queries * c->num_q_heads > (1 << 26))
+    return SKV_ERR_INVALID_ARG;
+  return SKV_OK;
+}
+
 }  // namespace
 }  // namespace skv
 
@@ -173,6 +216,85 @@ skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* r
     a.blocks = static_cast<uint32_t>(begin);
     return launch_attn_prompt(a, cfg->dtype, cfg->head_dim, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
   });
+}
+
+skv_status skv_attn_decode_workspace_size(const skv_decode_config* cfg, uint64_t* bytes) {
+  if (bytes == nullptr) return SKV_ERR_INVALID_ARG;
+  const skv_status st = check_decode_sizes(cfg);
+  if (st == SKV_OK) *bytes = plan_decode(cfg).part_bytes;
+  return st;
+}
+
+skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const void* k_cache, const void* v_cache,
+                           const int32_t* tables, const int32_t* lens, const uint8_t* tiers, void* out, float* lse,
+                           uint32_t* dev_status, void* ws, uint64_t ws_bytes, hipStream_t stream) {
+  skv_status st = check_decode_sizes(cfg);
+  if (st != SKV_OK) return st;
+  const skv_decode_config& c = *cfg;
+  if (!shape_ok(c.dtype, c.num_q_heads, c.num_kv_heads, c.head_dim, c.scale)) return SKV_ERR_INVALID_ARG;
+  if (c.num_blocks < 1 || c.block_size < 1 || static_cast<int64_t>(c.num_blocks) * c.block_size > INT32_MAX ||
+      c.table_width < 0 || static_cast<int64_t>(c.table_width) * c.block_size > INT32_MAX - 2 * 1024 ||
+      c.table_stride < c.table_width)
+    return SKV_ERR_INVALID_ARG;
+  if (c.prefix_len % c.block_size != 0 || c.prefix_len > c.table_width * c.block_size) return SKV_ERR_INVALID_ARG;
+  if (!stride_ok(c.q_request_stride) || !stride_ok(c.q_token_stride) || !stride_ok(c.q_head_stride) ||
+      !stride_ok(c.out_request_stride) || !stride_ok(c.out_token_stride) || !stride_ok(c.out_head_stride))
+    return SKV_ERR_INVALID_ARG;
+  if (tiers != nullptr && (c.tier_len < 0 || c.tier_request_stride < 0 || c.tier_head_stride < 0)) return SKV_ERR_INVALID_ARG;
+  if (c.num_requests == 0) return SKV_OK;
+  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(lens, 4) ||
+      !aligned(tables, 4) || (lse != nullptr && !aligned(lse, 4)) || (dev_status != nullptr && !aligned(dev_status, 4)))
+    return SKV_ERR_INVALID_ARG;
+  const DecodePlan p = plan_decode(cfg);
+  if (p.part_bytes > 0 && !aligned(ws, 16)) return SKV_ERR_INVALID_ARG;
+  if (ws_bytes < p.part_bytes || p.groups > kMaxGridThreads / 256) return SKV_ERR_CAPACITY;
+  const int32_t H = c.num_kv_heads, G = c.num_q_heads / H;
+  const uint64_t part_rows = static_cast<uint64_t>(p.prefix_parts + p.tail_parts) * c.num_requests * c.num_queries * c.num_q_heads;
+  DecodeArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k_cache);
+  a.v = static_cast<const uint16_t*>(v_cache);
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.tables = tables;
+  a.lens = lens;
+  a.tiers = tiers;
+  a.status = dev_status;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = p.part_bytes > 0 ? a.part_o + part_rows * static_cast<uint64_t>(c.head_dim) : nullptr;
+  a.q_request = c.q_request_stride;
+  a.q_token = c.q_token_stride;
+  a.q_head = c.q_head_stride;
+  a.out_request = c.out_request_stride;
+  a.out_token = c.out_token_stride;
+  a.out_head = c.out_head_stride;
+  a.table_stride = c.table_stride;
+  a.tier_request = c.tier_request_stride;
+  a.tier_head = c.tier_head_stride;
+  a.B = c.num_requests;
+  a.Lq = c.num_queries;
+  a.H = H;
+  a.G = G;
+  a.num_blocks = c.num_blocks;
+  a.block_size = c.block_size;
+  a.width = c.table_width;
+  a.prefix = c.prefix_len;
+  a.tier_len = c.tier_len;
+  a.prefix_parts = p.prefix_parts;
+  a.prefix_blocks = p.prefix_blocks;
+  a.prefix_tiles = p.prefix_tiles;
+  a.prefix_chunk = p.prefix_chunk;
+  a.tail_parts = p.tail_parts;
+  a.tail_blocks = p.tail_blocks;
+  a.tail_tiles = p.tail_tiles;
+  a.prefix_groups = static_cast<uint32_t>(p.prefix_groups);
+  a.groups = static_cast<uint32_t>(p.groups);
+  a.alpha = c.scale * kLog2e;
+  a.by_block = make_divider(static_cast<uint32_t>(c.block_size));
+  a.by_G = make_divider(static_cast<uint32_t>(G));
+  a.by_Lq = make_divider(static_cast<uint32_t>(c.num_queries));
+  return launch_attn_decode(a, c.dtype, c.head_dim, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
 }
 
 }  // extern "C"

@@ -40,4 +40,30 @@ static_assert(sizeof(PromptArgs) <= 4000, "kernel arguments");
 
 hipError_t launch_attn_prompt(const PromptArgs& a, int32_t dtype, int32_t d, hipStream_t stream);
 
+// Attention of a batch's newest tokens over the paged cache.  The launch's
+// workgroups are first those of the shared prefix (row blocks x KV heads x
+// parts, over the rows of every request), then those of the rest of each request
+// (requests x KV heads x parts x row blocks).
+struct DecodeArgs {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* out;
+  float* lse;             // [B][Lq][Hq], may be null
+  const int32_t* tables;  // [B][table_stride]
+  const int32_t* lens;
+  const uint8_t* tiers;   // may be null
+  uint32_t* status;       // may be null
+  float* part_o;          // [parts][H][B Lq G][d], unnormalized
+  float* part_ml;         // [parts][H][B Lq G][2]
+  int64_t q_request, q_token, q_head, out_request, out_token, out_head, table_stride, tier_request, tier_head;
+  int32_t B, Lq, H, G, num_blocks, block_size, width, prefix, tier_len;
+  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk;  // row blocks, 32-row tiles of one, tokens of a part
+  int32_t tail_parts, tail_blocks, tail_tiles;
+  uint32_t prefix_groups, groups;  // workgroups of the prefix, of the launch
+  float alpha;
+  Divider by_block, by_G, by_Lq;
+};
+hipError_t launch_attn_decode(const DecodeArgs& a, int32_t dtype, int32_t d, hipStream_t stream);
+
 }  // namespace skv

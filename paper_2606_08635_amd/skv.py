@@ -30,7 +30,8 @@ EXPORTED = ("skv_abi_version", "skv_status_string", "skv_plan_tiers", "skv_paylo
             "skv_pack_upgrade", "skv_unpack_upgrade", "skv_group_count", "skv_plan_groups",
             "skv_grouped_payload_size", "skv_group_workspace_size", "skv_prepare_groups", "skv_score_groups",
             "skv_assign_groups", "skv_pack_groups", "skv_unpack_groups", "skv_batch_workspace_size",
-            "skv_score_batch", "skv_assign_batch", "skv_attn_prompt_workspace_size", "skv_attn_prompt")
+            "skv_score_batch", "skv_assign_batch", "skv_attn_prompt_workspace_size", "skv_attn_prompt",
+            "skv_attn_decode_workspace_size", "skv_attn_decode")
 DTYPE_F16, DTYPE_BF16 = 0, 1
 
 
@@ -78,6 +79,15 @@ class AttnRequest(ctypes.Structure):
     _fields_ = [("num_queries", ctypes.c_int32), ("num_keys", ctypes.c_int32), ("q", ctypes.c_void_p),
                 ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
                 ("kv_token_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64)]
+
+
+class DecodeConfig(ctypes.Structure):
+    _fields_ = ([(name, ctypes.c_int32) for name in (
+        "dtype", "num_requests", "num_queries", "num_q_heads", "num_kv_heads", "head_dim", "num_blocks", "block_size",
+        "table_width", "max_len", "prefix_len", "tier_len")] + [("scale", ctypes.c_float)] +
+        [(name, ctypes.c_int64) for name in (
+            "q_request_stride", "q_token_stride", "q_head_stride", "out_request_stride", "out_token_stride",
+            "out_head_stride", "table_stride", "tier_request_stride", "tier_head_stride")])
 
 
 class Plan(ctypes.Structure):
@@ -131,6 +141,8 @@ def lib():
             "skv_score_batch": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, vp, vp]),
             "skv_assign_batch": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, vp, vp]),
             "skv_attn_prompt_workspace_size": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, P(u64)]),
+            "skv_attn_decode_workspace_size": (ctypes.c_int, [P(DecodeConfig), P(u64)]),
+            "skv_attn_decode": (ctypes.c_int, [P(DecodeConfig)] + [vp] * 10 + [u64, vp]),
             "skv_attn_prompt": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, vp, u64, vp]),
         }
         for name, (res, args) in sigs.items():
@@ -617,6 +629,72 @@ def attn_prompt(q: torch.Tensor, k, v, out: torch.Tensor, q_lens=None, kv_lens=N
     wsp = None if ws is None or ws.numel() == 0 else _dev(ws, torch.uint8, 0, "ws")
     _check(lib().skv_attn_prompt(ctypes.byref(cfg), reqs, count, wsp, 0 if wsp is None else ws.numel(),
                                  _stream(stream)), "skv_attn_prompt")
+
+
+def attn_decode_workspace_size(num_requests: int, num_queries: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                               max_len: int, prefix_len: int = 0) -> int:
+    """Workspace bytes of attn_decode with these arguments."""
+    cfg = DecodeConfig(num_requests=num_requests, num_queries=num_queries, num_q_heads=num_q_heads,
+                       num_kv_heads=num_kv_heads, head_dim=head_dim, max_len=max_len, prefix_len=prefix_len)
+    out = ctypes.c_uint64()
+    _check(lib().skv_attn_decode_workspace_size(ctypes.byref(cfg), ctypes.byref(out)),
+           "skv_attn_decode_workspace_size")
+    return out.value
+
+
+def attn_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor,
+                lens: torch.Tensor, out: torch.Tensor, ws: Optional[torch.Tensor], max_len: int, prefix_len: int = 0,
+                tiers: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                lse: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, stream=None):
+    """Attention of each request's newest tokens over one layer of a paged
+    cache.  q, out: [B][Lq][Hq][d] (any strides, last axis contiguous); k_cache,
+    v_cache: [num_blocks][block_size][H][d] (k_cache[layer] of what unpack
+    fills); block_tables: int32 [B][width]; lens: int32 [B], tokens in the cache,
+    the Lq newest among them.  max_len: about the longest length (sizes the
+    launch).  prefix_len: leading tokens that every request shares, a multiple
+    of the block size (their table entries and tiers are request 0's).  tiers:
+    uint8 [tier_len], [B][tier_len] or [B][H][tier_len] (expanded axes may
+    have stride 0); DROP tokens are masked, tokens past tier_len kept.  lse:
+    float32 [B][Lq][Hq].  ws: attn_decode_workspace_size bytes.  dev_status:
+    int32[1], set on a bad table entry or length, never cleared."""
+    if q.dtype not in _ATTN_TYPES:
+        raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
+    if q.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("q must be [B][Lq][Hq][d] and the caches [num_blocks][block_size][H][d]")
+    B, Lq, Hq, d = q.shape
+    nb, bs, H, _ = k_cache.shape
+    qp, op = _rows(q, q, q.shape, "q"), _rows(out, q, q.shape, "out")
+    kp = _dev(k_cache, q.dtype, nb * bs * H * d, "k_cache")
+    vp = _dev(v_cache, q.dtype, nb * bs * H * d, "v_cache")
+    if k_cache.shape != v_cache.shape or k_cache.shape[3] != d:
+        raise ValueError("caches must be [num_blocks][block_size][H][d] of q's d and alike")
+    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+        raise ValueError("block_tables must be [B][width]")
+    tp = _dev(block_tables, torch.int32, 0, "block_tables")
+    width = block_tables.shape[1]
+    if tiers is not None:
+        if not tiers.is_cuda or tiers.dtype != torch.uint8:
+            raise TypeError("tiers must be a uint8 device tensor")
+        n = tiers.shape[-1]
+        if tiers.dim() == 1:
+            tiers = tiers.expand(B, H, n)
+        elif tiers.dim() == 2:
+            tiers = tiers.unsqueeze(1).expand(B, H, n) if tiers.shape[0] == B else tiers
+        if tuple(tiers.shape) != (B, H, n):
+            raise ValueError("tiers must be [tier_len], [B][tier_len] or [B][H][tier_len]")
+        if n > 1 and tiers.stride(2) != 1:
+            raise ValueError("tiers' last axis must be contiguous")
+    cfg = DecodeConfig(_ATTN_TYPES[q.dtype], B, Lq, Hq, H, d, nb, bs, width, max_len, prefix_len,
+                       0 if tiers is None else tiers.shape[2], d ** -0.5 if scale is None else scale,
+                       _stride(q, 0), _stride(q, 1), _stride(q, 2), _stride(out, 0), _stride(out, 1), _stride(out, 2),
+                       width, 0 if tiers is None else tiers.stride(0), 0 if tiers is None else tiers.stride(1))
+    wsp = None if ws is None or ws.numel() == 0 else _dev(ws, torch.uint8, 0, "ws")
+    _check(lib().skv_attn_decode(
+        ctypes.byref(cfg), qp, kp, vp, tp, _dev(lens, torch.int32, B, "lens"),
+        None if tiers is None else tiers.data_ptr(), op,
+        None if lse is None else _dev(lse, torch.float32, B * Lq * Hq, "lse"),
+        None if dev_status is None else _dev(dev_status, torch.int32, 1, "dev_status"),
+        wsp, 0 if wsp is None else ws.numel(), _stream(stream)), "skv_attn_decode")
 
 
 def link(dst: torch.Tensor, src: torch.Tensor, nbytes: int, host_staging: Optional[torch.Tensor] = None,
