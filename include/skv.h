@@ -655,6 +655,77 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
                            const int32_t* tables, const int32_t* lens, const uint8_t* tiers, void* out, float* lse,
                            uint32_t* dev_status, void* ws, uint64_t ws_bytes, hipStream_t stream);
 
+/* Pages of the paged cache [L][num_blocks][block_size][H][d].  refs: int32
+ * [num_blocks], the number of block tables that hold each page; a page is free
+ * when it is 0 (the caller clears refs once; pages filled outside these calls get
+ * theirs set by the caller).  New pages are the lowest free ones, in (request,
+ * page) order.  Tables are int32 [requests][width], contiguous; a request of n
+ * tokens holds its table's first ceil(n / block_size) entries, and entries behind
+ * them are neither read nor written.  dev_status (required) is written by every
+ * call: 0; SKV_ERR_FORMAT for a length outside [0, width * block_size], a parent
+ * or page index out of range, or a held page whose count is 0; SKV_ERR_CAPACITY
+ * when too few pages are free or an output table is too narrow.  With a status
+ * other than 0 a call has changed nothing else (skv_pages_free excepted, see
+ * there).  ws: skv_pages_workspace_size bytes (ws_bytes; SKV_ERR_CAPACITY if less).
+ * Calls on one pool, and calls that share ws, must be ordered on one stream.
+ * Alignment 16 (k_cache, v_cache, refs, ws), 4 (int32 arrays, dev_status).  Kernel
+ * launches only: the calls can be captured in a HIP graph. */
+typedef struct skv_page_pool {
+  int32_t num_layers;  /* L                                                       */
+  int32_t num_blocks;  /* num_blocks * block_size < 2^31                           */
+  int32_t block_size;
+  int32_t row_bytes;   /* of one token of K (or V) in a layer, 2 H d: a multiple of 16 */
+  void* k_cache;       /* may be NULL for skv_pages_reserve and skv_pages_free     */
+  void* v_cache;
+  int32_t* refs;       /* not used by skv_pages_copy                               */
+} skv_page_pool;
+
+/* Host only.  Workspace bytes of the page calls on a pool of num_blocks pages with
+ * up to num_requests output rows whose tables hold up to max_len tokens (table
+ * width * block_size). */
+skv_status skv_pages_workspace_size(int32_t num_requests, int32_t num_blocks, int32_t max_len, uint64_t* bytes);
+
+/* Gives each request the pages that it needs to grow from lens to new_lens tokens
+ * (int32, device; none where new_lens is smaller) and writes them into its table. */
+skv_status skv_pages_reserve(const skv_page_pool* pool, int32_t* tables, int32_t table_width, const int32_t* lens,
+                             const int32_t* new_lens, int32_t num_requests, uint32_t* dev_status, void* ws,
+                             uint64_t ws_bytes, hipStream_t stream);
+
+/* Forks: child c becomes a copy of request parents[c] (a request may have several
+ * children).  Its full pages are shared (their counts go up by one per child); of
+ * a partly filled last page the child gets a page of its own, with the filled rows
+ * copied in every layer.  out_tables [num_children][out_width], out_lens
+ * int32[num_children]; they may not overlap tables and lens. */
+skv_status skv_pages_fork(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
+                          int32_t num_requests, const int32_t* parents, int32_t num_children, int32_t* out_tables,
+                          int32_t out_width, int32_t* out_lens, uint32_t* dev_status, void* ws, uint64_t ws_bytes,
+                          hipStream_t stream);
+
+/* Compaction: copies of the requests without their dropped tokens.  Token t of
+ * request b is dropped when t < tier_len and tiers[b * tier_stride + t] is
+ * SKV_TIER_DROP; the others keep their order.  Full pages before the first dropped
+ * token are shared as in a fork, the rows behind are gathered into new pages in
+ * every layer.  The source keeps its pages until skv_pages_free.  Positions change:
+ * a cold-tier upgrade names tokens by their old ones and belongs before.  The
+ * tables serve every layer and head, so one map per request. */
+skv_status skv_pages_compact(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
+                             int32_t num_requests, const uint8_t* tiers, int32_t tier_len, int64_t tier_stride,
+                             int32_t* out_tables, int32_t out_width, int32_t* out_lens, uint32_t* dev_status, void* ws,
+                             uint64_t ws_bytes, hipStream_t stream);
+
+/* Releases requests: the count of every page they hold goes down by one per entry.
+ * An entry out of range, a count that is 0 already and a bad length are passed
+ * over (dev_status SKV_ERR_FORMAT); everything else is released. */
+skv_status skv_pages_free(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
+                          int32_t num_requests, uint32_t* dev_status, hipStream_t stream);
+
+/* Copies page src_pages[i] of one pool to page dst_pages[i] of another (or of the
+ * same one), in every layer of K and V; the pools agree in layers, block size and
+ * row bytes.  Destinations must be distinct and not among the sources of the same
+ * pool. */
+skv_status skv_pages_copy(const skv_page_pool* src, const skv_page_pool* dst, const int32_t* src_pages,
+                          const int32_t* dst_pages, int32_t count, uint32_t* dev_status, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

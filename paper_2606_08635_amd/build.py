@@ -21,7 +21,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["skv_api.cpp", "score.hip", "attn.hip", "select.hip", "pack.hip", "unpack.hip", "upgrade.hip", "groups.hip",
            "link.hip", "serving/serving_api.cpp", "serving/attn_prompt.hip",
-           "serving/attn_decode.hip"]
+           "serving/attn_decode.hip", "serving/pages.hip"]
 FLAGS = [
     "-x", "hip", "-std=c++17", "-O3", "--offload-arch=gfx950", "-fPIC",
     "-ffp-contract=off", "-fhip-fp32-correctly-rounded-divide-sqrt",

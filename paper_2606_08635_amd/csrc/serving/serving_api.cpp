@@ -150,6 +150,90 @@ skv_status check_decode_sizes(const skv_decode_config* c) {
   return SKV_OK;
 }
 
+uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+// Workspace of the page operators: the status, five words per output row, the free
+// pages' list, two words per chunk of 256 tokens.
+struct PageLayout {
+  uint64_t rows, list, kept, first, total;
+  PageLayout(int64_t requests, int64_t blocks, int64_t chunks) {
+    rows = 256;
+    list = rows + 5 * up256(4u * static_cast<uint64_t>(requests));
+    kept = list + up256(4u * static_cast<uint64_t>(blocks));
+    first = kept + up256(4u * static_cast<uint64_t>(requests * chunks));
+    total = first + up256(4u * static_cast<uint64_t>(requests * chunks));
+  }
+};
+
+bool pool_ok(const skv_page_pool* p, bool caches, bool refs) {
+  return p != nullptr && p->num_layers >= 1 && p->num_layers <= 65536 && p->num_blocks >= 1 && p->block_size >= 1 &&
+         static_cast<int64_t>(p->num_blocks) * p->block_size <= INT32_MAX && p->row_bytes >= 16 &&
+         p->row_bytes % 16 == 0 && p->row_bytes <= (1 << 24) &&
+         (!caches || (aligned(p->k_cache, 16) && aligned(p->v_cache, 16))) && (!refs || aligned(p->refs, 16));
+}
+
+bool tables_ok(const skv_page_pool* p, const void* tables, int32_t width, const void* lens, int32_t requests) {
+  if (requests < 0 || width < 0 || static_cast<int64_t>(width) * p->block_size > (1 << 30) ||
+      static_cast<int64_t>(requests) * width > INT32_MAX)
+    return false;
+  return requests == 0 || (aligned(lens, 4) && (width == 0 || aligned(tables, 4)));
+}
+
+PageArgs page_args(const skv_page_pool* p, const int32_t* tables, int32_t width, const int32_t* lens, int32_t rows,
+                   uint32_t* status) {
+  PageArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.k = static_cast<uint8_t*>(p->k_cache);
+  a.v = static_cast<uint8_t*>(p->v_cache);
+  a.refs = p->refs;
+  a.tables = tables;
+  a.lens = lens;
+  a.status = status;
+  a.rows = rows;
+  a.sources = rows;
+  a.width = width;
+  a.num_blocks = p->num_blocks;
+  a.block_size = p->block_size;
+  a.num_layers = p->num_layers;
+  a.row_bytes = p->row_bytes;
+  a.plane_bytes = static_cast<int64_t>(p->num_blocks) * p->block_size * p->row_bytes;
+  a.chunks = 1;
+  a.plane_groups = 1;
+  a.by_block = make_divider(static_cast<uint32_t>(p->block_size));
+  a.by_units = make_divider(static_cast<uint32_t>(p->row_bytes / 16));
+  return a;
+}
+
+skv_status page_workspace(PageArgs* a, int64_t chunks, void* ws, uint64_t ws_bytes) {
+  const PageLayout lay(a->rows, a->num_blocks, chunks);
+  if (!aligned(ws, 16)) return SKV_ERR_INVALID_ARG;
+  if (ws_bytes < lay.total) return SKV_ERR_CAPACITY;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  const uint64_t row_area = up256(4u * static_cast<uint64_t>(a->rows));
+  auto at = [&](uint64_t off) { return reinterpret_cast<int32_t*>(base + off); };
+  a->ws_status = reinterpret_cast<uint32_t*>(base);
+  a->ws_bad = at(lay.rows);
+  a->ws_off = at(lay.rows + row_area);
+  a->ws_need = at(lay.rows + 2 * row_area);
+  a->ws_shared = at(lay.rows + 3 * row_area);
+  a->ws_total = at(lay.rows + 4 * row_area);
+  a->ws_list = at(lay.list);
+  a->ws_kept = at(lay.kept);
+  a->ws_first = at(lay.first);
+  return SKV_OK;
+}
+
+// Workgroups of the row copies: the planes are spread until the launch has about
+// `want` workgroups.
+skv_status spread_planes(PageArgs* a, int64_t pieces, int64_t want) {
+  const int64_t planes = 2 * static_cast<int64_t>(a->num_layers);
+  a->plane_groups = static_cast<int32_t>(std::max<int64_t>(1, std::min(planes, (want + pieces - 1) / pieces)));
+  const int64_t groups = pieces * a->plane_groups;
+  if (groups > static_cast<int64_t>(kMaxGridThreads / 256)) return SKV_ERR_CAPACITY;
+  a->copy_groups = static_cast<uint32_t>(groups);
+  return SKV_OK;
+}
+
 }  // namespace
 }  // namespace skv
 
@@ -295,6 +379,113 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   a.by_G = make_divider(static_cast<uint32_t>(G));
   a.by_Lq = make_divider(static_cast<uint32_t>(c.num_queries));
   return launch_attn_decode(a, c.dtype, c.head_dim, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
+}
+
+skv_status skv_pages_workspace_size(int32_t num_requests, int32_t num_blocks, int32_t max_len, uint64_t* bytes) {
+  if (bytes == nullptr || num_requests < 0 || num_blocks < 1 || max_len < 0 || max_len > (1 << 30)) return SKV_ERR_INVALID_ARG;
+  // (four chunks to spare: a table's last page may reach past max_len)
+  *bytes = PageLayout(num_requests, num_blocks, (static_cast<int64_t>(max_len) + 255) / 256 + 4).total;
+  return SKV_OK;
+}
+
+skv_status skv_pages_reserve(const skv_page_pool* pool, int32_t* tables, int32_t table_width, const int32_t* lens,
+                             const int32_t* new_lens, int32_t num_requests, uint32_t* dev_status, void* ws,
+                             uint64_t ws_bytes, hipStream_t stream) {
+  if (!pool_ok(pool, false, true) || !tables_ok(pool, tables, table_width, lens, num_requests) || !aligned(dev_status, 4) ||
+      (num_requests > 0 && !aligned(new_lens, 4)))
+    return SKV_ERR_INVALID_ARG;
+  PageArgs a = page_args(pool, tables, table_width, lens, num_requests, dev_status);
+  a.op = kPagesReserve;
+  a.new_lens = new_lens;
+  a.out_tables = tables;
+  a.out_width = table_width;
+  const skv_status st = page_workspace(&a, 0, ws, ws_bytes);
+  if (st != SKV_OK) return st;
+  return launch_pages(a, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
+}
+
+skv_status skv_pages_fork(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
+                          int32_t num_requests, const int32_t* parents, int32_t num_children, int32_t* out_tables,
+                          int32_t out_width, int32_t* out_lens, uint32_t* dev_status, void* ws, uint64_t ws_bytes,
+                          hipStream_t stream) {
+  if (!pool_ok(pool, true, true) || !tables_ok(pool, tables, table_width, lens, num_requests) ||
+      !tables_ok(pool, out_tables, out_width, out_lens, num_children) || !aligned(dev_status, 4) ||
+      (num_children > 0 && !aligned(parents, 4)))
+    return SKV_ERR_INVALID_ARG;
+  PageArgs a = page_args(pool, tables, table_width, lens, num_children, dev_status);
+  a.op = kPagesFork;
+  a.sources = num_requests;
+  a.parents = parents;
+  a.out_tables = out_tables;
+  a.out_width = out_width;
+  a.out_lens = out_lens;
+  // one workgroup looks over 16384 entries in about 5 us, less than a launch more costs
+  a.checked = static_cast<int64_t>(num_children) * table_width > 16384;
+  skv_status st = page_workspace(&a, 0, ws, ws_bytes);
+  if (st == SKV_OK) st = spread_planes(&a, std::max(1, num_children), 1024);
+  if (st != SKV_OK) return st;
+  if (num_children == 0) a.copy_groups = 0;
+  return launch_pages(a, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
+}
+
+skv_status skv_pages_compact(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
+                             int32_t num_requests, const uint8_t* tiers, int32_t tier_len, int64_t tier_stride,
+                             int32_t* out_tables, int32_t out_width, int32_t* out_lens, uint32_t* dev_status, void* ws,
+                             uint64_t ws_bytes, hipStream_t stream) {
+  if (!pool_ok(pool, true, true) || !tables_ok(pool, tables, table_width, lens, num_requests) ||
+      !tables_ok(pool, out_tables, out_width, out_lens, num_requests) || !aligned(dev_status, 4) || tier_len < 0 ||
+      tier_stride < 0 || (num_requests > 0 && tier_len > 0 && tiers == nullptr))
+    return SKV_ERR_INVALID_ARG;
+  PageArgs a = page_args(pool, tables, table_width, lens, num_requests, dev_status);
+  a.op = kPagesCompact;
+  a.tiers = tiers;
+  a.tier_len = tier_len;
+  a.tier_stride = tier_stride;
+  a.out_tables = out_tables;
+  a.out_width = out_width;
+  a.out_lens = out_lens;
+  a.chunks = static_cast<int32_t>(std::max<int64_t>(1, (static_cast<int64_t>(table_width) * pool->block_size + 255) / 256));
+  skv_status st = page_workspace(&a, a.chunks, ws, ws_bytes);
+  if (st == SKV_OK) st = spread_planes(&a, std::max<int64_t>(1, static_cast<int64_t>(num_requests) * a.chunks), 4096);
+  if (st != SKV_OK) return st;
+  if (num_requests == 0) a.copy_groups = 0;
+  return launch_pages(a, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
+}
+
+skv_status skv_pages_free(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
+                          int32_t num_requests, uint32_t* dev_status, hipStream_t stream) {
+  if (!pool_ok(pool, false, true) || !tables_ok(pool, tables, table_width, lens, num_requests) || !aligned(dev_status, 4))
+    return SKV_ERR_INVALID_ARG;
+  const PageArgs a = page_args(pool, tables, table_width, lens, num_requests, dev_status);
+  return launch_pages_free(a, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
+}
+
+skv_status skv_pages_copy(const skv_page_pool* src, const skv_page_pool* dst, const int32_t* src_pages,
+                          const int32_t* dst_pages, int32_t count, uint32_t* dev_status, hipStream_t stream) {
+  if (!pool_ok(src, true, false) || !pool_ok(dst, true, false) || src->num_layers != dst->num_layers ||
+      src->block_size != dst->block_size || src->row_bytes != dst->row_bytes || count < 0 || !aligned(dev_status, 4) ||
+      (count > 0 && (!aligned(src_pages, 4) || !aligned(dst_pages, 4))))
+    return SKV_ERR_INVALID_ARG;
+  PageCopyArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.src_k = static_cast<const uint8_t*>(src->k_cache);
+  a.src_v = static_cast<const uint8_t*>(src->v_cache);
+  a.dst_k = static_cast<uint8_t*>(dst->k_cache);
+  a.dst_v = static_cast<uint8_t*>(dst->v_cache);
+  a.src_pages = src_pages;
+  a.dst_pages = dst_pages;
+  a.status = dev_status;
+  a.page_bytes = static_cast<int64_t>(src->block_size) * src->row_bytes;
+  a.src_plane_bytes = a.page_bytes * src->num_blocks;
+  a.dst_plane_bytes = a.page_bytes * dst->num_blocks;
+  a.count = count;
+  a.src_blocks = src->num_blocks;
+  a.dst_blocks = dst->num_blocks;
+  a.planes = 2u * static_cast<uint32_t>(src->num_layers);
+  // workgroups of a launch sequence are numbered in 32 bits
+  if (static_cast<uint64_t>(count) * a.planes > UINT32_MAX / static_cast<uint64_t>((a.page_bytes + 32767) / 32768))
+    return SKV_ERR_CAPACITY;
+  return launch_pages_copy(a, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
 }
 
 }  // extern "C"

@@ -66,4 +66,53 @@ struct DecodeArgs {
 };
 hipError_t launch_attn_decode(const DecodeArgs& a, int32_t dtype, int32_t d, hipStream_t stream);
 
+// Page operators.  op kPagesReserve: tables grow in place (out_tables are the
+// tables, lens the old lengths); kPagesFork and kPagesCompact: out rows from
+// source rows (parents; null: row c from row c).
+enum { kPagesReserve = 0, kPagesFork = 1, kPagesCompact = 2 };
+struct PageArgs {
+  uint8_t* k;
+  uint8_t* v;
+  int32_t* refs;
+  const int32_t* tables;   // [sources][width]
+  const int32_t* lens;     // [sources]
+  const int32_t* new_lens; // reserve
+  const int32_t* parents;  // fork
+  const uint8_t* tiers;    // compact
+  int32_t* out_tables;     // [rows][out_width]
+  int32_t* out_lens;
+  uint32_t* status;
+  // workspace
+  uint32_t* ws_status;
+  int32_t* ws_bad;
+  int32_t* ws_off;
+  int32_t* ws_need;
+  int32_t* ws_shared;
+  int32_t* ws_total;
+  int32_t* ws_list;   // [num_blocks]
+  int32_t* ws_kept;   // [rows][chunks]: kept tokens of a chunk, then before it
+  int32_t* ws_first;  // [rows][chunks]: first dropped token
+  int64_t tier_stride, row_bytes, plane_bytes;
+  int32_t op, rows, sources, width, out_width, num_blocks, block_size, num_layers, tier_len;
+  int32_t chunks, plane_groups, checked;
+  uint32_t copy_groups;
+  Divider by_block, by_units;
+};
+hipError_t launch_pages(const PageArgs& a, hipStream_t stream);
+hipError_t launch_pages_free(const PageArgs& a, hipStream_t stream);
+
+struct PageCopyArgs {
+  const uint8_t* src_k;
+  const uint8_t* src_v;
+  uint8_t* dst_k;
+  uint8_t* dst_v;
+  const int32_t* src_pages;
+  const int32_t* dst_pages;
+  uint32_t* status;
+  int64_t page_bytes, src_plane_bytes, dst_plane_bytes;
+  int32_t count, src_blocks, dst_blocks;
+  uint32_t planes, pieces;
+};
+hipError_t launch_pages_copy(PageCopyArgs a, hipStream_t stream);
+
 }  // namespace skv

@@ -31,7 +31,8 @@ EXPORTED = ("skv_abi_version", "skv_status_string", "skv_plan_tiers", "skv_paylo
             "skv_grouped_payload_size", "skv_group_workspace_size", "skv_prepare_groups", "skv_score_groups",
             "skv_assign_groups", "skv_pack_groups", "skv_unpack_groups", "skv_batch_workspace_size",
             "skv_score_batch", "skv_assign_batch", "skv_attn_prompt_workspace_size", "skv_attn_prompt",
-            "skv_attn_decode_workspace_size", "skv_attn_decode")
+            "skv_attn_decode_workspace_size", "skv_attn_decode", "skv_pages_workspace_size", "skv_pages_reserve",
+            "skv_pages_fork", "skv_pages_compact", "skv_pages_free", "skv_pages_copy")
 DTYPE_F16, DTYPE_BF16 = 0, 1
 
 
@@ -90,6 +91,12 @@ class DecodeConfig(ctypes.Structure):
             "out_head_stride", "table_stride", "tier_request_stride", "tier_head_stride")])
 
 
+class PagePool(ctypes.Structure):
+    _fields_ = [("num_layers", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32),
+                ("row_bytes", ctypes.c_int32), ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p)]
+
+
 class Plan(ctypes.Structure):
     _fields_ = [("n_sink", ctypes.c_int32), ("n_fp16", ctypes.c_int32),
                 ("n_int8", ctypes.c_int32), ("n_int4", ctypes.c_int32),
@@ -143,6 +150,13 @@ def lib():
             "skv_attn_prompt_workspace_size": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, P(u64)]),
             "skv_attn_decode_workspace_size": (ctypes.c_int, [P(DecodeConfig), P(u64)]),
             "skv_attn_decode": (ctypes.c_int, [P(DecodeConfig)] + [vp] * 10 + [u64, vp]),
+            "skv_pages_workspace_size": (ctypes.c_int, [i32, i32, i32, P(u64)]),
+            "skv_pages_reserve": (ctypes.c_int, [P(PagePool), vp, i32, vp, vp, i32, vp, vp, u64, vp]),
+            "skv_pages_fork": (ctypes.c_int, [P(PagePool), vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, u64, vp]),
+            "skv_pages_compact": (ctypes.c_int, [P(PagePool), vp, i32, vp, i32, vp, i32, ctypes.c_int64, vp, i32, vp,
+                                                 vp, vp, u64, vp]),
+            "skv_pages_free": (ctypes.c_int, [P(PagePool), vp, i32, vp, i32, vp, vp]),
+            "skv_pages_copy": (ctypes.c_int, [P(PagePool), P(PagePool), vp, vp, i32, vp, vp]),
             "skv_attn_prompt": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, vp, u64, vp]),
         }
         for name, (res, args) in sigs.items():
@@ -695,6 +709,108 @@ def attn_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, b
         None if lse is None else _dev(lse, torch.float32, B * Lq * Hq, "lse"),
         None if dev_status is None else _dev(dev_status, torch.int32, 1, "dev_status"),
         wsp, 0 if wsp is None else ws.numel(), _stream(stream)), "skv_attn_decode")
+
+
+def _pool(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: Optional[torch.Tensor]) -> PagePool:
+    """The pool of a 16-bit paged cache pair [L][num_blocks][block_size][H][d]."""
+    if k_cache.dim() != 5 or k_cache.shape != v_cache.shape:
+        raise ValueError("caches must be [L][num_blocks][block_size][H][d] and alike")
+    if k_cache.dtype not in _ATTN_TYPES:
+        raise TypeError(f"caches must be float16 or bfloat16, got {k_cache.dtype}")
+    L, nb, bs, H, d = k_cache.shape
+    n = k_cache.numel()
+    return PagePool(L, nb, bs, 2 * H * d, _dev(k_cache, k_cache.dtype, n, "k_cache"), _dev(v_cache, k_cache.dtype, n, "v_cache"),
+                    None if refs is None else _dev(refs, torch.int32, nb, "refs"))
+
+
+def _tables(tables: torch.Tensor, rows: int, name: str):
+    """Pointer and width of contiguous block tables int32 [rows][width]."""
+    if tables.dim() != 2 or tables.shape[0] != rows:
+        raise ValueError(f"{name} must be [{rows}][width]")
+    return _dev(tables, torch.int32, 0, name), tables.shape[1]
+
+
+def pages_workspace_size(num_requests: int, num_blocks: int, max_len: int) -> int:
+    """Workspace bytes of pages_reserve, pages_fork and pages_compact with up to
+    num_requests output rows of up to max_len tokens (table width * block size)."""
+    out = ctypes.c_uint64()
+    _check(lib().skv_pages_workspace_size(num_requests, num_blocks, max_len, ctypes.byref(out)),
+           "skv_pages_workspace_size")
+    return out.value
+
+
+def pages_reserve(refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, new_lens: torch.Tensor,
+                  block_size: int, ws: torch.Tensor, dev_status: torch.Tensor, stream=None):
+    """Gives each request the pages to grow from lens to new_lens tokens: the
+    lowest free ones (refs 0), written into tables (int32 [B][width])."""
+    B = lens.numel()
+    pool = PagePool(1, refs.numel(), block_size, 16, None, None, _dev(refs, torch.int32, 0, "refs"))
+    tp, width = _tables(tables, B, "tables")
+    _check(lib().skv_pages_reserve(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"),
+                                   _dev(new_lens, torch.int32, B, "new_lens"), B,
+                                   _dev(dev_status, torch.int32, 1, "dev_status"),
+                                   _dev(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)), "skv_pages_reserve")
+
+
+def pages_fork(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor,
+               lens: torch.Tensor, parents: torch.Tensor, out_tables: torch.Tensor, out_lens: torch.Tensor,
+               ws: torch.Tensor, dev_status: torch.Tensor, stream=None):
+    """Child c becomes a copy of request parents[c]: full pages shared, a partly
+    filled last page copied.  Writes out_tables [children][width] and out_lens."""
+    B, N = lens.numel(), parents.numel()
+    pool = _pool(k_cache, v_cache, refs)
+    tp, width = _tables(tables, B, "tables")
+    op, out_width = _tables(out_tables, N, "out_tables")
+    _check(lib().skv_pages_fork(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"), B,
+                                _dev(parents, torch.int32, N, "parents"), N, op, out_width,
+                                _dev(out_lens, torch.int32, N, "out_lens"),
+                                _dev(dev_status, torch.int32, 1, "dev_status"),
+                                _dev(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)), "skv_pages_fork")
+
+
+def pages_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor,
+                  lens: torch.Tensor, tiers: torch.Tensor, out_tables: torch.Tensor, out_lens: torch.Tensor,
+                  ws: torch.Tensor, dev_status: torch.Tensor, stream=None):
+    """Copies of the requests without their DROP tokens (tiers: uint8
+    [B][tier_len], any request stride; tokens past tier_len are kept): full
+    pages before the first dropped token shared, the other rows gathered into
+    new pages."""
+    B = lens.numel()
+    pool = _pool(k_cache, v_cache, refs)
+    tp, width = _tables(tables, B, "tables")
+    op, out_width = _tables(out_tables, B, "out_tables")
+    if not tiers.is_cuda or tiers.dtype != torch.uint8:
+        raise TypeError("tiers must be a uint8 device tensor")
+    if tiers.dim() != 2 or tiers.shape[0] != B or (tiers.shape[1] > 1 and tiers.stride(1) != 1):
+        raise ValueError("tiers must be [requests][tier_len], its last axis contiguous")
+    _check(lib().skv_pages_compact(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"), B,
+                                   tiers.data_ptr(), tiers.shape[1], tiers.stride(0), op, out_width,
+                                   _dev(out_lens, torch.int32, B, "out_lens"),
+                                   _dev(dev_status, torch.int32, 1, "dev_status"),
+                                   _dev(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)), "skv_pages_compact")
+
+
+def pages_free(refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, block_size: int,
+               dev_status: torch.Tensor, stream=None):
+    """Releases requests: the count of every page they hold goes down by one."""
+    B = lens.numel()
+    pool = PagePool(1, refs.numel(), block_size, 16, None, None, _dev(refs, torch.int32, 0, "refs"))
+    tp, width = _tables(tables, B, "tables")
+    _check(lib().skv_pages_free(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"), B,
+                                _dev(dev_status, torch.int32, 1, "dev_status"), _stream(stream)), "skv_pages_free")
+
+
+def pages_copy(src_k: torch.Tensor, src_v: torch.Tensor, dst_k: torch.Tensor, dst_v: torch.Tensor,
+               src_pages: torch.Tensor, dst_pages: torch.Tensor, dev_status: torch.Tensor, stream=None):
+    """Copies page src_pages[i] of one cache pair to page dst_pages[i] of another
+    in every layer."""
+    src, dst = _pool(src_k, src_v, None), _pool(dst_k, dst_v, None)
+    if src_k.shape[2:] != dst_k.shape[2:] or src_k.shape[0] != dst_k.shape[0] or src_k.dtype != dst_k.dtype:
+        raise ValueError("the caches must agree in layers, block size, heads, dimension and type")
+    n = src_pages.numel()
+    _check(lib().skv_pages_copy(ctypes.byref(src), ctypes.byref(dst), _dev(src_pages, torch.int32, n, "src_pages"),
+                                _dev(dst_pages, torch.int32, n, "dst_pages"), n,
+                                _dev(dev_status, torch.int32, 1, "dev_status"), _stream(stream)), "skv_pages_copy")
 
 
 def link(dst: torch.Tensor, src: torch.Tensor, nbytes: int, host_staging: Optional[torch.Tensor] = None,
