@@ -35,7 +35,7 @@ struct TypeF16 {
   typedef _Float16 elem;
   typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
   typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
-  static constexpr uint32_t kInf = 0x7C00u, kOne = 0x3C00u;
+  static constexpr uint16_t kInf = 0x7C00, kOne = 0x3C00;
   __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -44,7 +44,7 @@ struct TypeBF16 {
   typedef __bf16 elem;
   typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
   typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
-  static constexpr uint32_t kInf = 0x7F80u, kOne = 0x3F80u;
+  static constexpr uint16_t kInf = 0x7F80, kOne = 0x3F80;
   __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -122,6 +122,7 @@ struct WaveAttention {
   // inside binary16.  m is some earlier step's maximum, so what underflows
   // against it is negligible beside what is in the sum already.
   static constexpr float kHigh = 32768.0f;
+  static constexpr uint16_t kInf = E::kInf, kOne = E::kOne;
 
   vec8 q[kSteps];
   floatx16 o[kTiles];
@@ -156,10 +157,27 @@ struct WaveAttention {
     l = 0.0f;
   }
 
+  // Moves on to the other stage buffer where steps do not name it (D = 256: its
+  // offset is past the 16 bits of an LDS instruction).
+  __device__ __forceinline__ void move(int bytes) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) kaddr[s] += bytes;
+#pragma unroll
+    for (int dt = 0; dt < (kTiles < 4 ? kTiles : 4); ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) vaddr[dt][u] += bytes;
+    vrows += bytes;
+  }
+
   __device__ __forceinline__ void load_q(const void* row) {
     const uint8_t* p = static_cast<const uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4*>(p + 32 * s));
+    // waited for here: the compiler's own wait would sit in the tile loop, where it
+    // would also wait for the direct loads that it does not know of
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(q[s]));
   }
 
   __device__ static __forceinline__ u32x4 lds16(uint32_t addr) {
@@ -204,66 +222,85 @@ struct WaveAttention {
   // o += V^T P^T for keys with p != 0 alone: V's infinities and NaN are taken out
   // of the product and counted in products of their own, so that one that is
   // hidden from a row (p = 0) does not reach it.
+  // (p >= 0, so its bits are 0 exactly where it is.)
   template <int OFF>
   __device__ __forceinline__ void accumulate_safe(const u32x4 (&p)[2 * NS]) {
-    auto each = [](u32x4 x, auto f) {
-      u32x4 y;
-      y.x = f(x.x & 0xFFFFu) | f(x.x >> 16) << 16;
-      y.y = f(x.y & 0xFFFFu) | f(x.y >> 16) << 16;
-      y.z = f(x.z & 0xFFFFu) | f(x.z >> 16) << 16;
-      y.w = f(x.w & 0xFFFFu) | f(x.w >> 16) << 16;
-      return y;
-    };
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) {
       floatx16 pos{}, neg{};
 #pragma unroll
       for (int s = 0; s < 2 * NS; ++s) {
+        asm volatile("" ::: "memory");  // one operand at a time: this path is rare, its registers are not to cost the other
         const u32x4 a = v_operand<OFF>(dt, s);
-        const u32x4 seen = each(p[s], [](uint32_t w) { return (w & 0x7FFFu) ? E::kOne : 0u; });
-        const u32x4 fin = each(a, [](uint32_t w) { return (w & 0x7FFFu) >= E::kInf ? 0u : w; });
-        const u32x4 up = each(a, [](uint32_t w) { return (w & 0x7FFFu) >= E::kInf && w != (E::kInf | 0x8000u) ? E::kOne : 0u; });
-        const u32x4 down = each(a, [](uint32_t w) { return (w & 0x7FFFu) >= E::kInf && w != E::kInf ? E::kOne : 0u; });
+        u32x4 fin, up, down, seen;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u16x2 w = __builtin_bit_cast(u16x2, a[i]), mag = w & static_cast<uint16_t>(0x7FFF);
+          const u16x2 zero = {0, 0}, one = {1, 1};
+          const u16x2 odd = zero - __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, u16x2(kInf - 1)), one);
+          const u16x2 nan = zero - __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, u16x2(kInf)), one);
+          const u16x2 neg1 = zero - (w >> static_cast<uint16_t>(15));
+          const u16x2 in = zero - __builtin_elementwise_min(__builtin_bit_cast(u16x2, p[s][i]), one);
+          fin[i] = __builtin_bit_cast(uint32_t, w & ~odd);
+          up[i] = __builtin_bit_cast(uint32_t, odd & (nan | ~neg1) & u16x2(kOne));
+          down[i] = __builtin_bit_cast(uint32_t, odd & (nan | neg1) & u16x2(kOne));
+          seen[i] = __builtin_bit_cast(uint32_t, in & u16x2(kOne));
+        }
         o[dt] = E::mfma(__builtin_bit_cast(vec8, fin), __builtin_bit_cast(vec8, p[s]), o[dt]);
         pos = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), pos);
         neg = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), neg);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        if (pos[r] > 0.0f) o[dt][r] += INFINITY;
-        if (neg[r] > 0.0f) o[dt][r] -= INFINITY;
+        // a count of one or more becomes infinity, none 0 (compares would be 64 live masks)
+        o[dt][r] += pos[r] * 0x1p127f * 4.0f;
+        o[dt][r] -= neg[r] * 0x1p127f * 4.0f;
       }
     }
   }
 
   // One step: the wave's NS * 32 keys of the stage at byte offset OFF of the
-  // stage area.  visible(n, r): whether key mfma_row(r, hf) of tile n is seen by
-  // the lane's query; asked only where MASK.
-  template <int OFF, bool MASK, class Visible>
-  __device__ __forceinline__ void step(float alpha, Visible visible) {
+  // stage area.  mask: whether some key is hidden from some row; visible(n, r): is
+  // key mfma_row(r, hf) of tile n seen by the lane's query.
+  template <int OFF, class Visible>
+  __device__ __forceinline__ void step(float alpha, bool mask, Visible visible) {
     floatx16 x[NS];
 #pragma unroll
     for (int n = 0; n < NS; ++n) x[n] = floatx16{};
+    // operands kAhead products early, so that their LDS reads are behind the matrix units' work
+    constexpr int kAhead = 4;
+    {
+      constexpr int kAll = NS * kSteps;
+      u32x4 a[kAhead + 1];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
+      for (int i = 0; i < kAll + kAhead; ++i) {
+        if (i < kAll) a[i % (kAhead + 1)] = lds16(kaddr[i / NS] + static_cast<uint32_t>(OFF + i % NS * 32 * S::kPitch));
+        if (i >= kAhead) {
+          const int c = i - kAhead;
+          x[c % NS] = E::mfma(__builtin_bit_cast(vec8, a[c % (kAhead + 1)]), q[c / NS], x[c % NS]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (__builtin_expect(mask, 0)) {
 #pragma unroll
       for (int n = 0; n < NS; ++n)
-        x[n] = E::mfma(__builtin_bit_cast(vec8, lds16(kaddr[s] + static_cast<uint32_t>(OFF + n * 32 * S::kPitch))), q[s], x[n]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!visible(n, r)) x[n][r] = -INFINITY;
+    }
     float e[NS][16];
     float sum = 0.0f;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (MASK && !visible(n, r)) x[n][r] = -INFINITY;
-        e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -m));
-      }
+      for (int r = 0; r < 16; ++r) e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -m));
       float t[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) t[r] = e[n][r] + e[n][r + 8];
       sum += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
     }
-    if (__any(!(sum <= kHigh))) {
+    if (__builtin_expect(__any(!(sum <= kHigh)), 0)) {
       float top = -INFINITY;
 #pragma unroll
       for (int n = 0; n < NS; ++n)
@@ -293,18 +330,23 @@ struct WaveAttention {
       p[s].z = pack2<E>(f[4], f[5]);
       p[s].w = pack2<E>(f[6], f[7]);
     }
-    if constexpr (MASK) {
-      if (v_not_finite<OFF>()) {
-        accumulate_safe<OFF>(p);
-        return;
-      }
+    if (__builtin_expect(mask && v_not_finite<OFF>(), 0)) {
+      accumulate_safe<OFF>(p);
+      return;
     }
+    constexpr int kAll = 2 * NS * kTiles;
+    u32x4 a[kAhead + 1];
 #pragma unroll
-    for (int s = 0; s < 2 * NS; ++s)
-#pragma unroll
-      for (int dt = 0; dt < kTiles; ++dt)
-        o[dt] = E::mfma(__builtin_bit_cast(vec8, v_operand<OFF>(dt, s)), __builtin_bit_cast(vec8, p[s]), o[dt]);
+    for (int i = 0; i < kAll + kAhead; ++i) {
+      if (i < kAll) a[i % (kAhead + 1)] = v_operand<OFF>(i % kTiles, i / kTiles);
+      if (i >= kAhead) {
+        const int c = i - kAhead;
+        o[c % kTiles] = E::mfma(__builtin_bit_cast(vec8, a[c % (kAhead + 1)]), __builtin_bit_cast(vec8, p[c / kTiles]), o[c % kTiles]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
+
   // Adds the state that another wave left at `from` (write_state) to this one's.
   static constexpr int kStateBytes = (D / 2 + 2) * 256;  // per wave
   __device__ __forceinline__ void write_state(uint8_t* to) const {
@@ -360,6 +402,41 @@ struct WaveAttention {
             floatx4{o[dt][4 * h], o[dt][4 * h + 1], o[dt][4 * h + 2], o[dt][4 * h + 3]};
   }
 };
+
+// Walks tiles [t0, t1) of a workgroup: issue(t, b) starts the direct loads of tile
+// t into buffer b, tile(t, off) multiplies the tile at stage offset `off` (an
+// integral constant).  The next tile is in flight while one is multiplied, and one
+// barrier per tile orders both: when it is passed every wave has the tile and is
+// done with the buffer that the next loads fill.
+template <int D, class Wave, class Issue, class Tile>
+__device__ __forceinline__ void walk_tiles(Wave& w, int t0, int t1, Issue issue, Tile tile) {
+  constexpr int kBytes = Stage<D>::kBytes;
+  if (t0 < t1) issue(t0, 0);
+  if constexpr (2 * kBytes <= 65536) {  // both buffers within an instruction's offset
+    for (int t = t0; t < t1; t += 2) {
+      wait_direct_loads();
+      stage_barrier();
+      if (t + 1 < t1) issue(t + 1, 1);
+      tile(t, std::integral_constant<int, 0>{});
+      if (t + 1 >= t1) break;
+      wait_direct_loads();
+      stage_barrier();
+      if (t + 2 < t1) issue(t + 2, 0);
+      tile(t + 1, std::integral_constant<int, kBytes>{});
+    }
+  } else {
+    int by = kBytes;
+    for (int t = t0; t < t1; ++t) {
+      wait_direct_loads();
+      stage_barrier();
+      if (t + 1 < t1) issue(t + 1, (t + 1 - t0) & 1);
+      tile(t, std::integral_constant<int, 0>{});
+      w.move(by);
+      by = -by;
+    }
+    if (by < 0) w.move(by);  // back to the first buffer
+  }
+}
 
 __device__ __forceinline__ float inverse_or_zero(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 __device__ __forceinline__ float log_sum(float m, float l) {

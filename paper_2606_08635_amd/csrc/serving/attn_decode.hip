@@ -106,8 +106,8 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, List
         direct_load(vbase + off, to + S::kHalf);
       }
     };
-    auto tile = [&](int t, auto buffer) {
-      constexpr int OFF = decltype(buffer)::value * S::kBytes;
+    auto tile = [&](int t, auto offset) {
+      constexpr int OFF = decltype(offset)::value;
       constexpr int kUnit = 64 / KS;
       const int key0 = t * S::kKeys + ks * 32;
       if (!active || key0 >= count) return;
@@ -117,21 +117,9 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, List
       };
       bool mask = key0 + kUnit > count;
       if (cut && !mask) mask = __builtin_amdgcn_readfirstlane(lists.pos[key0 + kUnit - 1]) > wave_min;
-      if (mask) w.template step<OFF, true>(a.alpha, visible);
-      else w.template step<OFF, false>(a.alpha, visible);
+      w.template step<OFF>(a.alpha, mask, visible);
     };
-    if (nt > 0) issue(0, 0);
-    for (int t = 0; t < nt; t += 2) {
-      wait_direct_loads();
-      stage_barrier();
-      if (t + 1 < nt) issue(t + 1, 1);
-      tile(t, std::integral_constant<int, 0>{});
-      if (t + 1 >= nt) break;
-      wait_direct_loads();
-      stage_barrier();
-      if (t + 2 < nt) issue(t + 2, 0);
-      tile(t + 1, std::integral_constant<int, 1>{});
-    }
+    walk_tiles<D>(w, 0, nt, issue, tile);
   }
   if constexpr (KS > 1) {  // the waves that took the other keys of the same rows
     __syncthreads();

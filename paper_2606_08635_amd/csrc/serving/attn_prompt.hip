@@ -73,27 +73,15 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
       direct_load(vbase + first, off, to + S::kHalf);
     }
   };
-  auto tile = [&](int t, auto buffer) {
-    constexpr int OFF = decltype(buffer)::value * S::kBytes;
+  auto tile = [&](int t, auto offset) {
+    constexpr int OFF = decltype(offset)::value;
     const int key0 = t * S::kKeys + ks * 32;
     if (!active || key0 > wave_max) return;
     const int mine = limit - key0 - 4 * hf;  // visible: 32 n + 8 (r / 4) + r % 4 <= mine
     auto visible = [&](int n, int rr) { return 32 * n + 8 * (rr >> 2) + (rr & 3) <= mine; };
-    if (key0 + 64 / KS - 1 > wave_min) w.template step<OFF, true>(a.alpha, visible);
-    else w.template step<OFF, false>(a.alpha, visible);
+    w.template step<OFF>(a.alpha, key0 + 64 / KS - 1 > wave_min, visible);
   };
-  if (t0 < t1) issue(t0, 0);
-  for (int t = t0; t < t1; t += 2) {
-    wait_direct_loads();
-    stage_barrier();
-    if (t + 1 < t1) issue(t + 1, 1);
-    tile(t, std::integral_constant<int, 0>{});
-    if (t + 1 >= t1) break;
-    wait_direct_loads();
-    stage_barrier();
-    if (t + 2 < t1) issue(t + 2, 0);
-    tile(t + 1, std::integral_constant<int, 1>{});
-  }
+  walk_tiles<D>(w, t0, t1, issue, tile);
   if constexpr (KS > 1) {  // the waves that took the other keys of the same rows
     stage_barrier();
     if (ks == 1) w.write_state(stage + rt * Wave::kStateBytes);
