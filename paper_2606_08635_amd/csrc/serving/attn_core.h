@@ -17,10 +17,16 @@
 // staged once for all of them, and one token per request still gives G rows.
 //
 // Roundings: products exact, sums, m, l and o in binary32; the probabilities are
-// rounded (nearest even) to the inputs' 16-bit type for the second product --
-// the MFMA takes both operands in one type -- while l sums them unrounded; the
-// result is rounded once to the output type.
+// rounded (nearest even) to the inputs' 16-bit type for the second product -- the
+// MFMA takes both operands in one type -- while l sums them unrounded; the result
+// is rounded once to the output type.  A row that sees few keys would show that
+// rounding (over many it averages out), so where it costs little -- tiles that a
+// row's limit cuts, among them every row's last and so all of a short one's, and the
+// steps of small and of bandwidth-bound calls -- what the rounding left over is
+// rounded too and multiplied as a second term.
 #pragma once
+
+#include <type_traits>
 
 #include "../device_util.h"
 
@@ -91,7 +97,7 @@ __device__ __forceinline__ void stage_barrier() {
 // of 4 consecutive rows (swz differs in the bits that select the 64-byte group).
 template <int D>
 struct Stage {
-  static constexpr int kWaves = 4;
+  static constexpr int kWaves = D >= 256 ? 8 : 4;
   static constexpr int kThreads = kWaves * 64;
   static constexpr int kKeys = 64;
   static constexpr int kCpr = D / 8;
@@ -100,73 +106,112 @@ struct Stage {
   static constexpr int kBytes = 2 * kHalf;
   static constexpr int kPieces = kKeys * kCpr / kThreads;  // 16-byte loads of K per thread, and of V
   static constexpr int kRowStep = kThreads / kCpr;         // rows between a thread's pieces
-  // waves per SIMD that the registers allow: o and Q alone are 3 D / 4 registers
-  static constexpr int kWavesPerSimd = D >= 256 ? 1 : 2;
+  static constexpr int kWavesPerSimd = 2;                  // 256 registers each
   static_assert(kKeys * kCpr % kThreads == 0, "whole pieces per thread");
   __device__ static constexpr int swz(int r) {
     return D >= 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : D == 64 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
   }
 };
 
-// One wave's 32 query rows: state and arithmetic.  NS: 32-key tiles that it
-// takes per step.
-template <class E, int D, int NS>
+// How a workgroup's waves share a stage of two 32-key tiles.
+enum Form {
+  kBoth,  // a wave has 32 rows to itself and takes both tiles in one step
+  kOne,   // a tile per step: both in turn, or with two key streams one each of two
+          // waves with the same rows, whose results are added at the end
+  kPair   // D = 256, where o and Q of 32 rows would not fit a wave's registers: two
+          // waves share 32 rows, each forms the logits of one tile, they exchange
+          // their probabilities through shared memory, and each sums half of V's
+          // channels over both tiles
+};
+
+// Shared memory besides the stage.
+struct Area {
+  int32_t not_finite;  // whether a wave's result asks for the second walk (walk_tiles)
+};
+// kPair: probabilities [row tile][key tile][step][lane] (second terms two row tiles
+// on: with more than two row tiles there are none), rows' maxima and sums, whether
+// a wave's sum asks for a higher reference.
+struct PairArea : Area {
+  u32x4 p[4][2][2][64];
+  float top[4][2][32];
+  float l[4][2][32];
+  alignas(16) uint32_t raise[8];
+};
+template <Form F>
+struct AreaOf {
+  typedef skv::Area type;
+};
+template <>
+struct AreaOf<kPair> {
+  typedef PairArea type;
+};
+
+// One wave's 32 query rows: state and arithmetic.
+template <class E, int D, Form F>
 struct WaveAttention {
   typedef typename E::vec8 vec8;
+  typedef typename AreaOf<F>::type AreaType;
   typedef Stage<D> S;
-  static constexpr int kSteps = D / 16;  // MFMA steps of a logit
-  static constexpr int kTiles = D / 32;  // 32-channel tiles of o
+  static constexpr int kChannels = F == kPair ? D / 2 : D;  // of o, in this wave
+  static constexpr int kSteps = D / 16;                     // MFMA steps of a logit
+  static constexpr int kTiles = kChannels / 32;             // 32-channel tiles of o
+  static constexpr int NS = F == kBoth ? 2 : 1;             // 32-key tiles of a step's logits
+  static constexpr int kReads = kSteps < 8 ? kSteps : 8;    // distinct LDS addresses of a K row's chunks
   // A step is exponentiated against the current reference m first, without its
   // maximum; only where that gives a sum past kHigh (or a NaN: m still -inf) is
   // the maximum taken, m raised and o rescaled.  2^15 keeps every probability
   // inside binary16.  m is some earlier step's maximum, so what underflows
   // against it is negligible beside what is in the sum already.
   static constexpr float kHigh = 32768.0f;
-  static constexpr uint16_t kInf = E::kInf, kOne = E::kOne;
+  static constexpr uint16_t kInf = E::kInf, kOne1 = E::kOne;
+  static constexpr int kAhead = 4;  // operands read ahead of their products
 
   vec8 q[kSteps];
   floatx16 o[kTiles];
   float m, l;
-  uint32_t kaddr[kSteps];               // LDS addresses in the first stage buffer
-  uint32_t vaddr[kTiles < 4 ? kTiles : 4][2];
-  uint32_t vrows;                       // this lane's 16 bytes of the wave's V rows
+  uint32_t kaddr[kReads];  // LDS addresses in the first stage buffer
+  uint32_t vaddr[kTiles][2];
+  int tiles;               // row tiles of the workgroup
+  int rt, ks, streams;     // row tile, place among the waves that share its rows, how many do
 
-  // first: the wave's first key of a stage
-  __device__ __forceinline__ void init(const void* stage, int first) {
+  // row_tiles: 32-row tiles of the workgroup; key_streams: of kOne
+  __device__ __forceinline__ void init(const void* stage, int row_tiles, int key_streams) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, hf = lane >> 5, j = lane & 31, i = lane & 15, g = (lane >> 4) & 1;
-    const uint32_t base = lds_address(stage) + static_cast<uint32_t>(first * S::kPitch);
+    tiles = row_tiles;
+    rt = wave % tiles;
+    ks = wave / tiles;
+    streams = F == kPair ? 2 : F == kOne ? key_streams : 1;
+    const uint32_t base = lds_address(stage);
+    const uint32_t own = F == kPair ? base + static_cast<uint32_t>((ks & 1) * 32 * S::kPitch) : base;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      kaddr[s] = base + static_cast<uint32_t>(j * S::kPitch + 16 * ((2 * s + hf) ^ S::swz(j)));
+    for (int s = 0; s < kReads; ++s) {
+      kaddr[s] = own + static_cast<uint32_t>(j * S::kPitch + 16 * ((2 * s + hf) ^ S::swz(j)));
       asm volatile("" : "+v"(kaddr[s]));  // one register each: tile offsets become immediates
     }
+    const int half = F == kPair ? (ks & 1) * 16 : 0;  // first chunk of this wave's channels
 #pragma unroll
-    for (int dt = 0; dt < (kTiles < 4 ? kTiles : 4); ++dt)
+    for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int row = 8 * u + 4 * hf + (i >> 2);
-        const int chunk = 4 * dt + 2 * g + ((i & 3) >> 1);
+        const int chunk = half + 4 * dt + 2 * g + ((i & 3) >> 1);
         vaddr[dt][u] =
             base + static_cast<uint32_t>(S::kHalf + row * S::kPitch + 16 * (chunk ^ S::swz(row)) + 8 * (i & 1));
         asm volatile("" : "+v"(vaddr[dt][u]));
       }
-    vrows = base + static_cast<uint32_t>(S::kHalf + 16 * lane);
-#pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt) o[dt] = floatx16{};
-    m = -INFINITY;
-    l = 0.0f;
+    reset();
   }
 
   // Moves on to the other stage buffer where steps do not name it (D = 256: its
   // offset is past the 16 bits of an LDS instruction).
   __device__ __forceinline__ void move(int bytes) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) kaddr[s] += bytes;
+    for (int s = 0; s < kReads; ++s) kaddr[s] += bytes;
 #pragma unroll
-    for (int dt = 0; dt < (kTiles < 4 ? kTiles : 4); ++dt)
+    for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
       for (int u = 0; u < 2; ++u) vaddr[dt][u] += bytes;
-    vrows += bytes;
   }
 
   __device__ __forceinline__ void load_q(const void* row) {
@@ -184,16 +229,16 @@ struct WaveAttention {
     typedef __attribute__((address_space(3))) const u32x4* ptr;
     return *reinterpret_cast<ptr>(static_cast<uintptr_t>(addr));
   }
-  // channels 32 dt + lane % 32 of the 8 keys 16 s + {4 hf .. + 3, 8 + 4 hf .. + 3}
+  // channels 32 dt + lane % 32 (of this wave's) of the 8 keys 16 s + {4 hf .. + 3, 8 + 4 hf .. + 3}
   template <int OFF>
   __device__ __forceinline__ u32x4 v_operand(int dt, int s) const {
     typedef __attribute__((address_space(3))) shortx4* ptr;
     u32x4 a;
-    const uint32_t off = static_cast<uint32_t>(OFF + 16 * s * S::kPitch + (dt >> 2) * 256);
+    const uint32_t off = static_cast<uint32_t>(OFF + 16 * s * S::kPitch);
     const u32x2 lo = __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ptr>(static_cast<uintptr_t>(vaddr[dt & 3][0] + off))));
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ptr>(static_cast<uintptr_t>(vaddr[dt][0] + off))));
     const u32x2 hi = __builtin_bit_cast(
-        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ptr>(static_cast<uintptr_t>(vaddr[dt & 3][1] + off))));
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<ptr>(static_cast<uintptr_t>(vaddr[dt][1] + off))));
     a.x = lo.x;
     a.y = lo.y;
     a.z = hi.x;
@@ -209,44 +254,128 @@ struct WaveAttention {
       for (int r = 0; r < 16; ++r) o[dt][r] *= f;
   }
 
-  // Whether V holds an infinity or NaN in the wave's keys of this stage.
-  template <int OFF>
-  __device__ __forceinline__ bool v_not_finite() const {
-    uint32_t top = 0;
+  // x = K Q^T of N 32-key tiles at byte offset OFF of the stage.
+  template <int OFF, int N>
+  __device__ __forceinline__ void logits(floatx16 (&x)[N]) const {
 #pragma unroll
-    for (int u = 0; u < NS * 32 * S::kPitch / 1024; ++u)
-      top = max(top, absmax_bits8(lds16(vrows + static_cast<uint32_t>(OFF + 1024 * u))));
-    return __any(top >= E::kInf);
+    for (int n = 0; n < N; ++n) x[n] = floatx16{};
+    constexpr int kAll = N * kSteps;
+    u32x4 a[kAhead + 1];
+#pragma unroll
+    for (int i = 0; i < kAll + kAhead; ++i) {
+      if (i < kAll) {
+        const int s = i / N, n = i % N;
+        a[i % (kAhead + 1)] = lds16(kaddr[s % kReads] + static_cast<uint32_t>(OFF + n * 32 * S::kPitch + s / kReads * 256));
+      }
+      if (i >= kAhead) {
+        const int c = i - kAhead;
+        x[c % N] = E::mfma(__builtin_bit_cast(vec8, a[c % (kAhead + 1)]), q[c / N], x[c % N]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // e = 2^(alpha x - ref); returns the lane's sum.
+  template <int N>
+  __device__ __forceinline__ float exponentials(const floatx16 (&x)[N], float alpha, float ref, float (&e)[N][16]) const {
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -ref));
+      float t[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) t[r] = e[n][r] + e[n][r + 8];
+      sum += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+    }
+    return sum;
+  }
+  // The row's largest logit, times alpha (both lane-halves get it).
+  template <int N>
+  __device__ __forceinline__ float largest(const floatx16 (&x)[N], float alpha) const {
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
+    const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, top * alpha));
+    return fmaxf(__builtin_bit_cast(float, p.lo), __builtin_bit_cast(float, p.hi));
+  }
+  // Raises m to mn >= m; returns the value to exponentiate against (0 while nothing
+  // has been seen, so that every probability is 0).
+  __device__ __forceinline__ float raise(float mn) {
+    const float ref = mn == -INFINITY ? 0.0f : mn;
+    rescale(__builtin_amdgcn_exp2f(m - ref));
+    m = mn;
+    return ref;
+  }
+  // Probabilities as second-product operands, rounded to E.
+  template <int N>
+  __device__ static __forceinline__ void pack(const float (&e)[N][16], u32x4 (&p)[2 * N]) {
+#pragma unroll
+    for (int s = 0; s < 2 * N; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[s][i] = pack2<E>(e[s >> 1][8 * (s & 1) + 2 * i], e[s >> 1][8 * (s & 1) + 2 * i + 1]);
+  }
+  // What that rounding left over, rounded to E.
+  template <int N>
+  __device__ static __forceinline__ void pack_rest(const float (&e)[N][16], const u32x4 (&p)[2 * N], u32x4 (&rest)[2 * N]) {
+#pragma unroll
+    for (int s = 0; s < 2 * N; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t both = p[s][i];  // (a bit cast of a vector's element itself would take the first)
+        const floatx2 f = __builtin_convertvector(__builtin_bit_cast(typename E::vec2, both), floatx2);
+        rest[s][i] = pack2<E>(e[s >> 1][8 * (s & 1) + 2 * i] - f.x, e[s >> 1][8 * (s & 1) + 2 * i + 1] - f.y);
+      }
+  }
+
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) o[dt] = floatx16{};
+    m = -INFINITY;
+    l = 0.0f;
+  }
+  // Whether the sums hold an infinity or NaN.
+  __device__ __forceinline__ bool not_finite() const {
+    float t = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) t = __builtin_fmaf(o[dt][r], 0.0f, t);
+    return __any(!(t == 0.0f));
   }
 
   // o += V^T P^T for keys with p != 0 alone: V's infinities and NaN are taken out
   // of the product and counted in products of their own, so that one that is
-  // hidden from a row (p = 0) does not reach it.
-  // (p >= 0, so its bits are 0 exactly where it is.)
-  template <int OFF>
-  __device__ __forceinline__ void accumulate_safe(const u32x4 (&p)[2 * NS]) {
+  // hidden from a row (p = 0) does not reach it.  (p >= 0, so its bits are 0
+  // exactly where it is.)
+  template <int OFF, int P>
+  __device__ __forceinline__ void accumulate_safe(const u32x4 (&p)[P], const u32x4 (&rest)[P]) {
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) {
       floatx16 pos{}, neg{};
 #pragma unroll
-      for (int s = 0; s < 2 * NS; ++s) {
-        asm volatile("" ::: "memory");  // one operand at a time: this path is rare, its registers are not to cost the other
+      for (int s = 0; s < P; ++s) {
+        asm volatile("" ::: "memory");  // one operand at a time: registers
         const u32x4 a = v_operand<OFF>(dt, s);
         u32x4 fin, up, down, seen;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const u16x2 w = __builtin_bit_cast(u16x2, a[i]), mag = w & static_cast<uint16_t>(0x7FFF);
+          const uint32_t ai = a[i], pi = p[s][i];
+          const u16x2 w = __builtin_bit_cast(u16x2, ai), mag = w & static_cast<uint16_t>(0x7FFF);
           const u16x2 zero = {0, 0}, one = {1, 1};
           const u16x2 odd = zero - __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, u16x2(kInf - 1)), one);
           const u16x2 nan = zero - __builtin_elementwise_min(__builtin_elementwise_sub_sat(mag, u16x2(kInf)), one);
-          const u16x2 neg1 = zero - (w >> static_cast<uint16_t>(15));
-          const u16x2 in = zero - __builtin_elementwise_min(__builtin_bit_cast(u16x2, p[s][i]), one);
+          const u16x2 minus = zero - (w >> static_cast<uint16_t>(15));
+          const u16x2 in = zero - __builtin_elementwise_min(__builtin_bit_cast(u16x2, pi), one);
           fin[i] = __builtin_bit_cast(uint32_t, w & ~odd);
-          up[i] = __builtin_bit_cast(uint32_t, odd & (nan | ~neg1) & u16x2(kOne));
-          down[i] = __builtin_bit_cast(uint32_t, odd & (nan | neg1) & u16x2(kOne));
-          seen[i] = __builtin_bit_cast(uint32_t, in & u16x2(kOne));
+          up[i] = __builtin_bit_cast(uint32_t, odd & (nan | ~minus) & u16x2(kOne1));
+          down[i] = __builtin_bit_cast(uint32_t, odd & (nan | minus) & u16x2(kOne1));
+          seen[i] = __builtin_bit_cast(uint32_t, in & u16x2(kOne1));
         }
         o[dt] = E::mfma(__builtin_bit_cast(vec8, fin), __builtin_bit_cast(vec8, p[s]), o[dt]);
+        o[dt] = E::mfma(__builtin_bit_cast(vec8, fin), __builtin_bit_cast(vec8, rest[s]), o[dt]);
         pos = E::mfma(__builtin_bit_cast(vec8, up), __builtin_bit_cast(vec8, seen), pos);
         neg = E::mfma(__builtin_bit_cast(vec8, down), __builtin_bit_cast(vec8, seen), neg);
       }
@@ -259,29 +388,31 @@ struct WaveAttention {
     }
   }
 
-  // One step: the wave's NS * 32 keys of the stage at byte offset OFF of the
-  // stage area.  mask: whether some key is hidden from some row; visible(n, r): is
-  // key mfma_row(r, hf) of tile n seen by the lane's query.
-  template <int OFF, class Visible>
+  // o += V^T P^T of P 16-key steps at byte offset OFF; TWO: with the rest's product.
+  template <int OFF, bool TWO, int P>
+  __device__ __forceinline__ void accumulate(const u32x4 (&p)[P], const u32x4 (&rest)[P]) {
+    constexpr int kAll = P * kTiles;
+    u32x4 a[kAhead + 1];
+#pragma unroll
+    for (int i = 0; i < kAll + kAhead; ++i) {
+      if (i < kAll) a[i % (kAhead + 1)] = v_operand<OFF>(i % kTiles, i / kTiles);
+      if (i >= kAhead) {
+        const int c = i - kAhead;
+        const vec8 v = __builtin_bit_cast(vec8, a[c % (kAhead + 1)]);
+        o[c % kTiles] = E::mfma(v, __builtin_bit_cast(vec8, p[c / kTiles]), o[c % kTiles]);
+        if (TWO) o[c % kTiles] = E::mfma(v, __builtin_bit_cast(vec8, rest[c / kTiles]), o[c % kTiles]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // The NS key tiles at byte offset OFF of the stage.  mask: whether some key is
+  // hidden from some row; visible(n, r): whether the lane's query sees key
+  // mfma_row(r, hf) of the n-th.
+  template <int OFF, bool SECOND, class Visible>
   __device__ __forceinline__ void step(float alpha, bool mask, Visible visible) {
     floatx16 x[NS];
-#pragma unroll
-    for (int n = 0; n < NS; ++n) x[n] = floatx16{};
-    // operands kAhead products early, so that their LDS reads are behind the matrix units' work
-    constexpr int kAhead = 4;
-    {
-      constexpr int kAll = NS * kSteps;
-      u32x4 a[kAhead + 1];
-#pragma unroll
-      for (int i = 0; i < kAll + kAhead; ++i) {
-        if (i < kAll) a[i % (kAhead + 1)] = lds16(kaddr[i / NS] + static_cast<uint32_t>(OFF + i % NS * 32 * S::kPitch));
-        if (i >= kAhead) {
-          const int c = i - kAhead;
-          x[c % NS] = E::mfma(__builtin_bit_cast(vec8, a[c % (kAhead + 1)]), q[c / NS], x[c % NS]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
+    logits<OFF>(x);
     if (__builtin_expect(mask, 0)) {
 #pragma unroll
       for (int n = 0; n < NS; ++n)
@@ -290,65 +421,138 @@ struct WaveAttention {
           if (!visible(n, r)) x[n][r] = -INFINITY;
     }
     float e[NS][16];
-    float sum = 0.0f;
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -m));
-      float t[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) t[r] = e[n][r] + e[n][r + 8];
-      sum += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
-    }
-    if (__builtin_expect(__any(!(sum <= kHigh)), 0)) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
-      const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, top * alpha));
-      const float mn = fmaxf(m, fmaxf(__builtin_bit_cast(float, p.lo), __builtin_bit_cast(float, p.hi)));
-      const float ref = mn == -INFINITY ? 0.0f : mn;  // nothing seen yet: every probability 0
-      rescale(__builtin_amdgcn_exp2f(m - ref));
-      m = mn;
-      sum = 0.0f;
-#pragma unroll
-      for (int n = 0; n < NS; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          e[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][r], alpha, -ref));
-          sum += e[n][r];
-        }
-    }
+    float sum = exponentials(x, alpha, m, e);
+    if (__builtin_expect(__any(!(sum <= kHigh)), 0)) sum = exponentials(x, alpha, raise(fmaxf(m, largest(x, alpha))), e);
     l += sum;
-    u32x4 p[2 * NS];
-#pragma unroll
-    for (int s = 0; s < 2 * NS; ++s) {
-      const float* f = &e[s >> 1][8 * (s & 1)];
-      p[s].x = pack2<E>(f[0], f[1]);
-      p[s].y = pack2<E>(f[2], f[3]);
-      p[s].z = pack2<E>(f[4], f[5]);
-      p[s].w = pack2<E>(f[6], f[7]);
-    }
-    if (__builtin_expect(mask && v_not_finite<OFF>(), 0)) {
-      accumulate_safe<OFF>(p);
-      return;
-    }
-    constexpr int kAll = 2 * NS * kTiles;
-    u32x4 a[kAhead + 1];
-#pragma unroll
-    for (int i = 0; i < kAll + kAhead; ++i) {
-      if (i < kAll) a[i % (kAhead + 1)] = v_operand<OFF>(i % kTiles, i / kTiles);
-      if (i >= kAhead) {
-        const int c = i - kAhead;
-        o[c % kTiles] = E::mfma(__builtin_bit_cast(vec8, a[c % (kAhead + 1)]), __builtin_bit_cast(vec8, p[c / kTiles]), o[c % kTiles]);
+    u32x4 p[2 * NS], rest[2 * NS];
+    pack(e, p);
+    if constexpr (SECOND) {
+      pack_rest(e, p, rest);
+      accumulate_safe<OFF>(p, rest);
+    } else if constexpr (F == kOne) {
+      pack_rest(e, p, rest);
+      accumulate<OFF, true>(p, rest);
+    } else {
+      accumulate<OFF, false>(p, p);
+      if (__builtin_expect(mask, 0)) {
+        pack_rest(e, p, rest);
+        accumulate<OFF, false>(rest, rest);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
-  // Adds the state that another wave left at `from` (write_state) to this one's.
-  static constexpr int kStateBytes = (D / 2 + 2) * 256;  // per wave
+  // kPair: both tiles of the stage; every wave of the workgroup calls it.  on:
+  // whether this wave's rows see any of it; fine: two-term probabilities.
+  template <bool SECOND, class Visible>
+  __device__ __forceinline__ void step_pair(AreaType& area, float alpha, bool on, bool mask, bool fine, Visible visible) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int tile = ks & 1;  // (a wave past the pairs has no rows: on is false)
+    fine = (fine || mask) && tiles <= 2;
+    floatx16 x[1];
+    float e[1][16], sum = 0.0f;
+    auto give = [&] {
+      u32x4 p[2];
+      pack(e, p);
+      area.p[rt][tile][0][lane] = p[0];
+      area.p[rt][tile][1][lane] = p[1];
+      if (fine) {
+        u32x4 rest[2];
+        pack_rest(e, p, rest);
+        area.p[rt + 2][tile][0][lane] = rest[0];
+        area.p[rt + 2][tile][1][lane] = rest[1];
+      }
+    };
+    bool high = false;
+    if (__builtin_expect(on, 1)) {
+      logits<0>(x);
+      if (__builtin_expect(mask, 0)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!visible(tile, r)) x[0][r] = -INFINITY;
+      }
+      sum = exponentials(x, alpha, m, e);
+      high = __any(!(sum <= kHigh));
+      give();
+    }
+    if (lane == 0) area.raise[wave] = high;
+    stage_barrier();
+    const u32x4 f0 = *reinterpret_cast<const u32x4*>(area.raise), f1 = *reinterpret_cast<const u32x4*>(area.raise + 4);
+    if (__builtin_expect(__any((f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w) != 0), 0)) {
+      // both waves of a pair go on against one reference
+      const float top = on ? largest(x, alpha) : -INFINITY;
+      if (on && lane < 32) area.top[rt][tile][lane] = top;
+      stage_barrier();
+      if (on) {
+        sum = exponentials(x, alpha, raise(fmaxf(m, fmaxf(area.top[rt][0][lane & 31], area.top[rt][1][lane & 31]))), e);
+        give();
+      }
+      stage_barrier();
+    }
+    if (__builtin_expect(!on, 0)) return;
+    l += sum;
+    u32x4 p[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) p[s] = area.p[rt][s >> 1][s & 1][lane];
+    u32x4 rest[4];
+    if constexpr (SECOND) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) rest[s] = fine ? area.p[rt + 2][s >> 1][s & 1][lane] : u32x4{};
+      accumulate_safe<0>(p, rest);
+    } else {
+      accumulate<0, false>(p, p);
+      if (__builtin_expect(fine, 0)) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) rest[s] = area.p[rt + 2][s >> 1][s & 1][lane];
+        accumulate<0, false>(rest, rest);
+      }
+    }
+  }
+
+  // The stage at byte offset OFF.  first_key: of the stage; masked(key, keys):
+  // whether some of these keys is hidden from some row; shown(key): whether the
+  // lane's query sees it.
+  template <int OFF, bool SECOND, class Masked, class Shown>
+  __device__ __forceinline__ void tile(AreaType& area, float alpha, int first_key, bool on, bool fine, Masked masked,
+                                       Shown shown) {
+    const int hf = (threadIdx.x >> 5) & 1;
+    auto visible = [&](int n, int r) { return shown(first_key + 32 * n + mfma_row(r, hf)); };
+    if constexpr (F == kPair) {
+      step_pair<SECOND>(area, alpha, on && ks < 2, on && masked(first_key, 64), fine, visible);
+    } else if constexpr (F == kBoth) {
+      if (on && ks == 0) step<OFF, SECOND>(alpha, masked(first_key, 64), visible);
+    } else if (on && ks < streams) {
+      if (streams == 1 || ks == 0) step<OFF, SECOND>(alpha, masked(first_key, 32), visible);
+      if (streams == 1 || ks == 1)
+        step<OFF + 32 * S::kPitch, SECOND>(alpha, masked(first_key + 32, 32), [&](int, int r) { return visible(1, r); });
+    }
+  }
+
+  // Adds up what the waves that share rows have; every wave calls it, after the
+  // last tile.  Returns whether this wave writes (kPair: its channels), with l the
+  // row's sum.
+  static constexpr int kStateBytes = (kChannels / 2 + 2) * 256;  // per wave
+  __device__ __forceinline__ bool finish(uint8_t* stage, AreaType& area, bool on) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (F == kOne) {
+      if (streams == 2) {
+        stage_barrier();
+        uint8_t* at = stage + rt * kStateBytes;
+        if (on && ks == 1) write_state(at);
+        stage_barrier();
+        if (on && ks == 0) merge_state(at);
+      }
+    }
+    {
+      const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, l));
+      l = __builtin_bit_cast(float, p.lo) + __builtin_bit_cast(float, p.hi);
+    }
+    if constexpr (F == kPair) {
+      if (on && ks < 2) area.l[rt][ks][lane & 31] = l;
+      stage_barrier();
+      if (on && ks < 2) l = area.l[rt][0][lane & 31] + area.l[rt][1][lane & 31];
+    }
+    return on && ks < (F == kPair ? 2 : 1);
+  }
   __device__ __forceinline__ void write_state(uint8_t* to) const {
     float* f = reinterpret_cast<float*>(to) + (threadIdx.x & 63);
     f[0] = m;
@@ -369,14 +573,11 @@ struct WaveAttention {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[dt][r] = o[dt][r] * a + f[64 * (2 + 16 * dt + r)] * b;
   }
-  // l over both lane-halves.
-  __device__ __forceinline__ float total() const {
-    const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, l));
-    return __builtin_bit_cast(float, p.lo) + __builtin_bit_cast(float, p.hi);
-  }
+  // Whether this lane writes the row's reference and sum, or its lse.
+  __device__ __forceinline__ bool writes_sum() const { return (threadIdx.x & 32) == 0 && ks == 0; }
   // The row's result, rounded to E: a lane-half writes 16 contiguous bytes.
   __device__ __forceinline__ void write_out(void* row, float inv) const {
-    uint8_t* p = static_cast<uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1);
+    uint8_t* p = static_cast<uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1) + (F == kPair ? ks * D : 0);
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
@@ -393,7 +594,7 @@ struct WaveAttention {
   }
   // The row's unnormalized sum in binary32.
   __device__ __forceinline__ void write_partial(float* row) const {
-    float* p = row + 4 * ((threadIdx.x >> 5) & 1);
+    float* p = row + 4 * ((threadIdx.x >> 5) & 1) + (F == kPair ? ks * kChannels : 0);
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
@@ -404,25 +605,26 @@ struct WaveAttention {
 };
 
 // Walks tiles [t0, t1) of a workgroup: issue(t, b) starts the direct loads of tile
-// t into buffer b, tile(t, off) multiplies the tile at stage offset `off` (an
-// integral constant).  The next tile is in flight while one is multiplied, and one
-// barrier per tile orders both: when it is passed every wave has the tile and is
-// done with the buffer that the next loads fill.
-template <int D, class Wave, class Issue, class Tile>
-__device__ __forceinline__ void walk_tiles(Wave& w, int t0, int t1, Issue issue, Tile tile) {
+// t into buffer b, tile(t, off, second) multiplies the tile at stage offset `off`
+// (integral constants).  The next tile is in flight while one is multiplied, and
+// one barrier per tile orders both: when it is passed every wave has the tile and
+// is done with the buffer that the next loads fill.
+template <int D, bool SECOND, class Wave, class Issue, class Tile>
+__device__ __forceinline__ void walk_once(Wave& w, int t0, int t1, Issue issue, Tile tile) {
   constexpr int kBytes = Stage<D>::kBytes;
+  const std::integral_constant<bool, SECOND> second;
   if (t0 < t1) issue(t0, 0);
   if constexpr (2 * kBytes <= 65536) {  // both buffers within an instruction's offset
     for (int t = t0; t < t1; t += 2) {
       wait_direct_loads();
       stage_barrier();
       if (t + 1 < t1) issue(t + 1, 1);
-      tile(t, std::integral_constant<int, 0>{});
+      tile(t, std::integral_constant<int, 0>{}, second);
       if (t + 1 >= t1) break;
       wait_direct_loads();
       stage_barrier();
       if (t + 2 < t1) issue(t + 2, 0);
-      tile(t + 1, std::integral_constant<int, kBytes>{});
+      tile(t + 1, std::integral_constant<int, kBytes>{}, second);
     }
   } else {
     int by = kBytes;
@@ -430,11 +632,29 @@ __device__ __forceinline__ void walk_tiles(Wave& w, int t0, int t1, Issue issue,
       wait_direct_loads();
       stage_barrier();
       if (t + 1 < t1) issue(t + 1, (t + 1 - t0) & 1);
-      tile(t, std::integral_constant<int, 0>{});
+      tile(t, std::integral_constant<int, 0>{}, second);
       w.move(by);
       by = -by;
     }
     if (by < 0) w.move(by);  // back to the first buffer
+  }
+}
+// walk(second) goes through all of a workgroup's tiles (walk_once).  The products of
+// the first time let an infinity or NaN of V reach rows from which it is hidden (0
+// times it is NaN), and second terms make NaN of one that is seen; so where a result
+// is not finite, everything is done again by accumulate_safe, whose arithmetic would
+// cost the first loop its registers.  Ends with a barrier: the stage is free.
+template <class Wave, class AreaType, class Walk>
+__device__ __forceinline__ void walk_tiles(Wave& w, AreaType& area, Walk walk) {
+  if (threadIdx.x == 0) area.not_finite = 0;
+  walk(std::integral_constant<bool, false>{});
+  stage_barrier();
+  if (w.not_finite()) area.not_finite = 1;
+  stage_barrier();
+  if (__builtin_expect(*const_cast<volatile int32_t*>(&area.not_finite) != 0, 0)) {
+    w.reset();
+    walk(std::integral_constant<bool, true>{});
+    stage_barrier();
   }
 }
 

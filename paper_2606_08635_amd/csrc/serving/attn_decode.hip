@@ -17,24 +17,27 @@
 namespace skv {
 namespace {
 
-constexpr int kList = 1024;  // positions listed at a time: 4 per thread
+constexpr int kList = 1024;  // positions listed at a time
 
+template <int THREADS>
 struct Lists {
   int32_t rows[kList];  // row of the cache: page * block_size + slot
-  int32_t pos[kList];   // token position
-  uint32_t scan[4];
-  int32_t count;
+  int32_t pos[kList];   // token position; past the list's end, to the end of its last tile, one that nothing sees
+  uint32_t scan[THREADS / 64];
 };
 
 // The kept positions of [p0, p1), p1 - p0 <= kList, in order.  The caller's
 // barrier before the call has ended every use of the previous list.
-__device__ __forceinline__ int build_list(const DecodeArgs& a, Lists& s, const int32_t* table, const uint8_t* tier, int p0,
-                                          int p1) {
-  int32_t row[4], n = 0;
-  const int first = p0 + 4 * static_cast<int>(threadIdx.x);
+template <int THREADS>
+__device__ __forceinline__ int build_list(const DecodeArgs& a, Lists<THREADS>& s, const int32_t* table, const uint8_t* tier,
+                                          int p0, int p1) {
+  constexpr int kPer = kList / THREADS;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int32_t row[kPer], n = 0;
+  const int first = p0 + kPer * static_cast<int>(threadIdx.x);
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kPer; ++i) {
     const int p = first + i;
     row[i] = -1;
     if (p >= p1) continue;
@@ -46,30 +49,41 @@ __device__ __forceinline__ int build_list(const DecodeArgs& a, Lists& s, const i
     n += row[i] >= 0;
   }
   if (bad && a.status != nullptr) *a.status = SKV_ERR_FORMAT;
-  int to = static_cast<int>(block_exclusive_scan_256(static_cast<uint32_t>(n), s.scan));
-  if (threadIdx.x == 255) s.count = to + n;
+  const uint32_t inc = wave_inclusive_scan(static_cast<uint32_t>(n));
+  if (lane == 63) s.scan[wave] = inc;
+  __syncthreads();
+  int to = static_cast<int>(inc) - n, count = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int w = 0; w < THREADS / 64; ++w) {
+    if (w < wave) to += static_cast<int>(s.scan[w]);
+    count += static_cast<int>(s.scan[w]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
     if (row[i] >= 0) {
       s.rows[to] = row[i];
       s.pos[to] = first + i;
       ++to;
     }
+  const int past = count + static_cast<int>(threadIdx.x);
+  if (past < (count + 63) / 64 * 64) s.pos[past] = INT32_MAX;
   __syncthreads();
-  return s.count;
+  return __builtin_amdgcn_readfirstlane(count);
 }
 
 // Rows [row0, row0 + rows) of the launch's B Lq G (row = (request * Lq + query) *
 // G + head of the group) against positions [p0, p1) of `table`.
-template <class E, int D, int KS>
-__device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, Lists& lists, int h, int row0, int rows, int tiles,
-                                       const int32_t* table, const uint8_t* tier, int p0, int p1, int part, bool only) {
+template <class E, int D, Form F>
+__device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, typename WaveAttention<E, D, F>::AreaType& area,
+                                       Lists<Stage<D>::kThreads>& lists, int h, int row0, int rows, int tiles, const int32_t* table,
+                                       const uint8_t* tier, int p0, int p1, int part, bool only) {
   typedef Stage<D> S;
-  typedef WaveAttention<E, D, 2 / KS> Wave;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
-  const int rt = wave % tiles, ks = wave / tiles;
-  const bool active = ks < KS && rt * 32 < rows;
-  const int mine = rt * 32 + (lane & 31);
+  typedef WaveAttention<E, D, F> Wave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Wave w;
+  w.init(stage, tiles, tiles == 4 ? 1 : 2);
+  const bool active = w.rt * 32 < rows;
+  const int mine = w.rt * 32 + (lane & 31);
   const uint32_t row = static_cast<uint32_t>(row0 + min(mine, rows - 1));
   const uint32_t token = a.by_G.div(row), g = row - token * a.G;
   const uint32_t b = a.by_Lq.div(token), i = token - b * a.Lq;
@@ -81,69 +95,60 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, List
   for (int x = 16; x > 0; x >>= 1) wave_min = min(wave_min, __shfl_xor(wave_min, x));
   wave_min = __builtin_amdgcn_readfirstlane(wave_min);
 
-  Wave w;
-  w.init(stage, ks * 32);
   w.load_q(a.q + b * a.q_request + i * a.q_token + head * a.q_head);
   const int prow = static_cast<int>(threadIdx.x) / S::kCpr, place = static_cast<int>(threadIdx.x) % S::kCpr;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(stage) + static_cast<uint32_t>(wave * 1024));
   const int64_t cache_row = static_cast<int64_t>(a.H) * D;
   const uint16_t* kbase = a.k + h * D;
   const uint16_t* vbase = a.v + h * D;
-  for (int q0 = p0; q0 < p1; q0 += kList) {
-    const int q1 = min(p1, q0 + kList);
-    if (q0 > p0) __syncthreads();
-    const int count = build_list(a, lists, table, tier, q0, q1);
-    const int nt = (count + S::kKeys - 1) / S::kKeys;
-    const bool cut = q1 - 1 > wave_min;  // some row ends before the list does
-    auto issue = [&](int t, int buffer) {
+  walk_tiles(w, area, [&](auto second) {
+    for (int q0 = p0; q0 < p1; q0 += kList) {
+      const int q1 = min(p1, q0 + kList);
+      const int count = build_list(a, lists, table, tier, q0, q1);
+      const int nt = (count + S::kKeys - 1) / S::kKeys;
+      const bool cut = q1 - 1 > wave_min;  // some row ends before the list does
+      auto issue = [&](int t, int buffer) {
 #pragma unroll
-      for (int u = 0; u < S::kPieces; ++u) {
-        const int rr = prow + u * S::kRowStep;
-        // rows past the list's end repeat its last one: hidden from every row
-        const int64_t off = lists.rows[min(t * S::kKeys + rr, count - 1)] * cache_row + 8 * (place ^ S::swz(rr));
-        const uint32_t to = lds0 + static_cast<uint32_t>(buffer * S::kBytes + u * S::kThreads * 16);
-        direct_load(kbase + off, to);
-        direct_load(vbase + off, to + S::kHalf);
-      }
-    };
-    auto tile = [&](int t, auto offset) {
-      constexpr int OFF = decltype(offset)::value;
-      constexpr int kUnit = 64 / KS;
-      const int key0 = t * S::kKeys + ks * 32;
-      if (!active || key0 >= count) return;
-      auto visible = [&](int n, int r) {
-        const int at = key0 + 32 * n + mfma_row(r, hf);
-        return at < count && lists.pos[min(at, count - 1)] <= limit;
+        for (int u = 0; u < S::kPieces; ++u) {
+          const int rr = prow + u * S::kRowStep;
+          // rows past the list's end repeat its last one: hidden from every row
+          const int64_t off = lists.rows[min(t * S::kKeys + rr, count - 1)] * cache_row + 8 * (place ^ S::swz(rr));
+          const uint32_t to = lds0 + static_cast<uint32_t>(buffer * S::kBytes + u * S::kThreads * 16);
+          direct_load(kbase + off, to);
+          direct_load(vbase + off, to + S::kHalf);
+        }
       };
-      bool mask = key0 + kUnit > count;
-      if (cut && !mask) mask = __builtin_amdgcn_readfirstlane(lists.pos[key0 + kUnit - 1]) > wave_min;
-      w.template step<OFF>(a.alpha, mask, visible);
-    };
-    walk_tiles<D>(w, 0, nt, issue, tile);
-  }
-  if constexpr (KS > 1) {  // the waves that took the other keys of the same rows
-    __syncthreads();
-    if (active && ks == 1) w.write_state(stage + rt * Wave::kStateBytes);
-    __syncthreads();
-    if (ks != 0) return;
-    if (active) w.merge_state(stage + rt * Wave::kStateBytes);
-  }
-  if (!active || mine >= rows) return;
-  const float l = w.total();
+      auto masked = [&](int key, int keys) {
+        if (key + keys > count) return true;
+        return cut && __builtin_amdgcn_readfirstlane(lists.pos[key + keys - 1]) > wave_min;
+      };
+      auto shown = [&](int key) { return lists.pos[key] <= limit; };
+      auto tile = [&](int t, auto offset, auto again) {
+        w.template tile<decltype(offset)::value, decltype(again)::value>(area, a.alpha, t * S::kKeys, active, true, masked,
+                                                                          shown);
+      };
+      walk_once<D, decltype(second)::value>(w, 0, nt, issue, tile);
+      if (q1 < p1) __syncthreads();  // the next list
+    }
+  });
+  const bool writes = w.finish(stage, area, active);
+  if (!writes || mine >= rows) return;
   if (only) {
-    w.write_out(a.out + b * a.out_request + i * a.out_token + head * a.out_head, inverse_or_zero(l));
-    if (a.lse != nullptr && hf == 0) a.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, l);
+    w.write_out(a.out + b * a.out_request + i * a.out_token + head * a.out_head, inverse_or_zero(w.l));
+    if (a.lse != nullptr && w.writes_sum()) a.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, w.l);
     return;
   }
   const int64_t at = (static_cast<int64_t>(part) * a.H + h) * (static_cast<int64_t>(a.B) * a.Lq * a.G) + row;
   if (p0 < p1) w.write_partial(a.part_o + at * D);
-  if (hf == 0) *reinterpret_cast<floatx2*>(a.part_ml + 2 * at) = floatx2{w.m, l};
+  if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * at) = floatx2{w.m, w.l};
 }
 
 template <class E, int D>
 __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void attn_decode(const DecodeArgs a) {
+  constexpr Form F = D >= 256 ? kPair : kOne;
   __shared__ __align__(1024) uint8_t stage[2 * Stage<D>::kBytes];
-  __shared__ Lists lists;
+  __shared__ typename WaveAttention<E, D, F>::AreaType area;
+  __shared__ Lists<Stage<D>::kThreads> lists;
   uint32_t at = blockIdx.x;
   const uint32_t H = static_cast<uint32_t>(a.H);
   int h, row0, rows, tiles, p0, p1, part;
@@ -183,8 +188,7 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
     tier = a.tiers == nullptr ? nullptr : a.tiers + b * a.tier_request + h * a.tier_head;
   }
   const bool only = a.prefix_parts + a.tail_parts == 1;
-  if (tiles == 4) attend<E, D, 1>(a, stage, lists, h, row0, rows, tiles, table, tier, p0, p1, part, only);
-  else attend<E, D, 2>(a, stage, lists, h, row0, rows, tiles, table, tier, p0, p1, part, only);
+  attend<E, D, F>(a, stage, area, lists, h, row0, rows, tiles, table, tier, p0, p1, part, only);
 }
 
 // Joins the parts of each row: one wave per (KV head, row).

@@ -17,11 +17,12 @@
 namespace skv {
 namespace {
 
-template <class E, int D, int KS>
+template <class E, int D, Form F>
 __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void attn_prompt(const PromptArgs a) {
   typedef Stage<D> S;
-  typedef WaveAttention<E, D, 2 / KS> Wave;
+  typedef WaveAttention<E, D, F> Wave;
   __shared__ __align__(1024) uint8_t stage[2 * S::kBytes];
+  __shared__ typename Wave::AreaType area;
   const uint32_t block = blockIdx.x;
   int ri = 0;
   for (int step = 32; step > 0; step >>= 1)  // the last request that begins at or before this workgroup
@@ -35,10 +36,11 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
   const int blk = nblk - 1 - static_cast<int>(at / static_cast<uint32_t>(r.splits));
   const int split = static_cast<int>(at % static_cast<uint32_t>(r.splits));
 
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hf = lane >> 5;
-  const int rt = wave % a.row_tiles, ks = wave / a.row_tiles;
-  const int row0 = blk * per + rt * 32;  // the wave's first row
-  const bool active = ks < KS && row0 < rows;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Wave w;
+  w.init(stage, a.row_tiles, a.key_streams);
+  const int row0 = blk * per + w.rt * 32;  // the wave's first row
+  const bool active = row0 < rows;
   const int row = min(row0 + (lane & 31), rows - 1);
   const int token = row / a.G, head = h * a.G + row % a.G;
   const int more = r.nk - r.nq;
@@ -50,8 +52,6 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
   const int t0 = static_cast<int>(static_cast<int64_t>(all) * split / r.splits);
   const int t1 = static_cast<int>(static_cast<int64_t>(all) * (split + 1) / r.splits);
 
-  Wave w;
-  w.init(stage, ks * 32);
   w.load_q(r.q + token * a.q_token + head * a.q_head);
 
   // this thread's pieces of a stage: row tid / kCpr + u * kRowStep, place tid % kCpr
@@ -73,32 +73,23 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
       direct_load(vbase + first, off, to + S::kHalf);
     }
   };
-  auto tile = [&](int t, auto offset) {
-    constexpr int OFF = decltype(offset)::value;
-    const int key0 = t * S::kKeys + ks * 32;
-    if (!active || key0 > wave_max) return;
-    const int mine = limit - key0 - 4 * hf;  // visible: 32 n + 8 (r / 4) + r % 4 <= mine
-    auto visible = [&](int n, int rr) { return 32 * n + 8 * (rr >> 2) + (rr & 3) <= mine; };
-    w.template step<OFF>(a.alpha, key0 + 64 / KS - 1 > wave_min, visible);
+  auto tile = [&](int t, auto offset, auto second) {
+    const int key0 = t * S::kKeys;
+    w.template tile<decltype(offset)::value, decltype(second)::value>(
+        area, a.alpha, key0, active && key0 <= wave_max, false, [&](int key, int keys) { return key + keys - 1 > wave_min; },
+        [&](int key) { return key <= limit; });
   };
-  walk_tiles<D>(w, t0, t1, issue, tile);
-  if constexpr (KS > 1) {  // the waves that took the other keys of the same rows
-    stage_barrier();
-    if (ks == 1) w.write_state(stage + rt * Wave::kStateBytes);
-    stage_barrier();
-    if (ks != 0) return;
-    w.merge_state(stage + rt * Wave::kStateBytes);
-  }
-  if (!active || row0 + (lane & 31) >= rows) return;  // (both lane-halves of a row stay: total and write_out pair them)
-  const float l = w.total();
+  walk_tiles(w, area, [&](auto second) { walk_once<D, decltype(second)::value>(w, t0, t1, issue, tile); });
+  const bool writes = w.finish(stage, area, active);
+  if (!writes || row0 + (lane & 31) >= rows) return;  // (both lane-halves of a row stay: write_out pairs them)
   if (r.splits > 1) {
     const int64_t prow_at = r.rows_at + (static_cast<int64_t>(split) * a.H + h) * rows + row;
     w.write_partial(a.part_o + prow_at * D);
-    if (hf == 0) *reinterpret_cast<floatx2*>(a.part_ml + 2 * prow_at) = floatx2{w.m, l};
+    if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * prow_at) = floatx2{w.m, w.l};
     return;
   }
-  w.write_out(r.out + token * a.out_token + head * a.out_head, inverse_or_zero(l));
-  if (r.lse != nullptr && hf == 0) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, l);
+  w.write_out(r.out + token * a.out_token + head * a.out_head, inverse_or_zero(w.l));
+  if (r.lse != nullptr && w.writes_sum()) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, w.l);
 }
 
 // Joins the parts of requests with splits > 1: one wave per row.
@@ -118,8 +109,9 @@ __global__ __launch_bounds__(256) void attn_prompt_join(const PromptArgs a, int 
 
 template <class E, int D>
 hipError_t launch(const PromptArgs& a, hipStream_t stream) {
-  if (a.key_streams == 1) attn_prompt<E, D, 1><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
-  else attn_prompt<E, D, 2><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
+  if constexpr (D >= 256) attn_prompt<E, D, kPair><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
+  else if (a.key_streams == 1) attn_prompt<E, D, kBoth><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
+  else attn_prompt<E, D, kOne><<<a.blocks, Stage<D>::kThreads, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   for (int i = 0; i < a.count && e == hipSuccess; ++i) {
     if (a.r[i].splits <= 1) continue;

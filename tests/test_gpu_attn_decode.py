@@ -1,7 +1,6 @@
 """Decode attention over a paged cache against its definition in float64:
 types, head layouts, drafted tokens, block sizes, shared prefixes, dropped
 tokens, empty and short requests, bad tables, streams and graphs."""
-import numpy as np
 import pytest
 import torch
 
@@ -126,3 +125,92 @@ def test_empty_requests():
     out, lse = b.run()
     assert (out[1] == 0).all() and (lse[1] == -float("inf")).all()
     check(out, lse, b.want())
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+def test_hidden_values_have_no_effect(d):
+    """Infinities and NaN in dropped tokens reach nothing, in drafted tokens only the later drafts; in the prefix only
+    the requests that reach them."""
+    b = Batch([600, 530, 500], 4, 2, d, Lq=4, prefix=512, tier_len=520, drop=0.3, seed=d)
+    for x in (b.k, b.v):
+        for r, t in zip(b.rows, b.tiers):
+            m = min(len(r), len(t))
+            x[r[:m][t[:m] == skv.DROP]] = float("nan")
+    b.v[b.rows[0][-1]], b.v[b.rows[1][-2], 0, 5] = float("nan"), float("inf")
+    b.tiers[:, 505:512] = 0
+    b.v[b.rows[0][506], :, 3] = float("-inf")  # past request 2's end
+    for x in (b.k, b.v):
+        x[b.rows[0][507:512]] = torch.where(torch.isnan(x[b.rows[0][507:512]]), 0.5, x[b.rows[0][507:512]])
+        x[b.rows[0][505:506]] = 0.25
+    b.k[b.rows[0][506]] = 0.25
+    check(*b.run(), b.want(), d)
+
+
+def test_bad_tables_and_lengths():
+    b = Batch([300, 200], 4, 2, 64, seed=8)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    want = b.run(status=status)
+    assert status.item() == 0
+    tables = b.tables.clone()
+    tables[0, 2], tables[1, 3], tables[1, 15:] = -1, b.shape[0], 1 << 30  # two in use, one behind the end
+    out, lse = b.run(tables=tables, status=status)
+    assert status.item() == skv.ERR_FORMAT
+    cut = Batch([300, 200], 4, 2, 64, seed=8, tier_len=300)
+    cut.tiers[:] = 0
+    cut.tiers[0, 32:48] = cut.tiers[1, 48:64] = skv.DROP  # their tokens are left out
+    check(out, lse, cut.want(), "bad entries")
+    status.zero_()
+    tables = b.tables.clone()
+    tables[1, 13:] = 1 << 30
+    out, lse = b.run(tables=tables, status=status)
+    assert status.item() == 0 and torch.equal(out, want[0])
+    out, lse = b.run(lens=[-5, 1 << 20], status=status)
+    assert status.item() == skv.ERR_FORMAT
+    assert (out[0] == 0).all()
+
+
+def test_strides_and_stream():
+    b = Batch([300, 40, 7], 8, 2, 128, Lq=2, tier_len=100, drop=0.5, head_maps=True, seed=4)
+    want = b.want()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    check(*b.run(stream=s), want, "stream")
+    q = torch.full((3, 2, 10, 136), 7.0, dtype=torch.float16, device=DEV)
+    q[:, :, 1:9, :128] = b.q.to(DEV)
+    out = torch.full((2, 9, 3, 128), 7.0, dtype=torch.float16, device=DEV)
+    tiers = torch.zeros(3, 4, 2, 107, dtype=torch.uint8, device=DEV)[:, 1, :, 3:103]
+    tiers.copy_(b.tiers.to(DEV))
+    lse = torch.empty(3, 2, 8, device=DEV)
+    ws = torch.empty(skv.attn_decode_workspace_size(3, 2, 8, 2, 128, 300), dtype=torch.uint8, device=DEV)
+    skv.attn_decode(q[:, :, 1:9, :128], b.k.view(b.shape).to(DEV), b.v.view(b.shape).to(DEV), b.tables.to(DEV),
+                    torch.tensor(b.lens, dtype=torch.int32, device=DEV), out[:, :8].permute(2, 0, 1, 3), ws, 300,
+                    tiers=tiers, lse=lse)
+    check(out[:, :8].permute(2, 0, 1, 3), lse, want, "strided")
+    assert (out[:, 8] == 7.0).all()
+
+
+def test_graph_follows_lengths_and_tables():
+    """Captured once; replayed with other lengths, queries and tables, eager work between."""
+    b = Batch([500, 300], 8, 2, 128, prefix=128, seed=12)
+    q, k, v = b.q.to(DEV), b.k.view(b.shape).to(DEV), b.v.view(b.shape).to(DEV)
+    tables, lens = b.tables.to(DEV), torch.tensor(b.lens, dtype=torch.int32, device=DEV)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device=DEV)
+    need = skv.attn_decode_workspace_size(2, 1, 8, 2, 128, 500, 128)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        skv.attn_decode(q, k, v, tables, lens, out, ws, 500, prefix_len=128, lse=lse)
+    for i, now in enumerate(([500, 300], [130, 200], [499, 1])):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        q.normal_()
+        if i == 1:
+            tables[:, 8:] = tables[:, 8:].flip(0).clone()
+        want, want_lse = torch.empty_like(out), torch.empty_like(lse)
+        skv.attn_decode(q, k, v, tables, lens, want, torch.empty_like(ws), 500, prefix_len=128, lse=want_lse)
+        torch.cuda.synchronize()
+        out.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        # bit for bit: the last replay's first request reads rows that hold NaN
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+        assert torch.equal(lse.view(torch.int32), want_lse.view(torch.int32))
