@@ -218,8 +218,11 @@ struct WaveAttention {
     const uint8_t* p = static_cast<const uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4*>(p + 32 * s));
-    // waited for here: the compiler's own wait would sit in the tile loop, where it
-    // would also wait for the direct loads that it does not know of
+  }
+  // Waits for Q; to be called before the first direct load.  The compiler's own wait
+  // would sit in the tile loop, where it would also wait for the direct loads that it
+  // does not know of.
+  __device__ __forceinline__ void wait_q() {
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(q[s]));
@@ -388,9 +391,9 @@ struct WaveAttention {
     }
   }
 
-  // o += V^T P^T of P 16-key steps at byte offset OFF; TWO: with the rest's product.
-  template <int OFF, bool TWO, int P>
-  __device__ __forceinline__ void accumulate(const u32x4 (&p)[P], const u32x4 (&rest)[P]) {
+  // o += V^T P^T of P 16-key steps at byte offset OFF.
+  template <int OFF, int P>
+  __device__ __forceinline__ void accumulate(const u32x4 (&p)[P]) {
     constexpr int kAll = P * kTiles;
     u32x4 a[kAhead + 1];
 #pragma unroll
@@ -398,9 +401,7 @@ struct WaveAttention {
       if (i < kAll) a[i % (kAhead + 1)] = v_operand<OFF>(i % kTiles, i / kTiles);
       if (i >= kAhead) {
         const int c = i - kAhead;
-        const vec8 v = __builtin_bit_cast(vec8, a[c % (kAhead + 1)]);
-        o[c % kTiles] = E::mfma(v, __builtin_bit_cast(vec8, p[c / kTiles]), o[c % kTiles]);
-        if (TWO) o[c % kTiles] = E::mfma(v, __builtin_bit_cast(vec8, rest[c / kTiles]), o[c % kTiles]);
+        o[c % kTiles] = E::mfma(__builtin_bit_cast(vec8, a[c % (kAhead + 1)]), __builtin_bit_cast(vec8, p[c / kTiles]), o[c % kTiles]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -408,9 +409,9 @@ struct WaveAttention {
 
   // The NS key tiles at byte offset OFF of the stage.  mask: whether some key is
   // hidden from some row; visible(n, r): whether the lane's query sees key
-  // mfma_row(r, hf) of the n-th.
+  // mfma_row(r, hf) of the n-th; fine: two-term probabilities.
   template <int OFF, bool SECOND, class Visible>
-  __device__ __forceinline__ void step(float alpha, bool mask, Visible visible) {
+  __device__ __forceinline__ void step(float alpha, bool mask, bool fine, Visible visible) {
     floatx16 x[NS];
     logits<OFF>(x);
     if (__builtin_expect(mask, 0)) {
@@ -429,14 +430,11 @@ struct WaveAttention {
     if constexpr (SECOND) {
       pack_rest(e, p, rest);
       accumulate_safe<OFF>(p, rest);
-    } else if constexpr (F == kOne) {
-      pack_rest(e, p, rest);
-      accumulate<OFF, true>(p, rest);
     } else {
-      accumulate<OFF, false>(p, p);
-      if (__builtin_expect(mask, 0)) {
+      accumulate<OFF>(p);
+      if (__builtin_expect(fine || mask, F == kOne)) {
         pack_rest(e, p, rest);
-        accumulate<OFF, false>(rest, rest);
+        accumulate<OFF>(rest);
       }
     }
   }
@@ -499,11 +497,11 @@ struct WaveAttention {
       for (int s = 0; s < 4; ++s) rest[s] = fine ? area.p[rt + 2][s >> 1][s & 1][lane] : u32x4{};
       accumulate_safe<0>(p, rest);
     } else {
-      accumulate<0, false>(p, p);
+      accumulate<0>(p);
       if (__builtin_expect(fine, 0)) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) rest[s] = area.p[rt + 2][s >> 1][s & 1][lane];
-        accumulate<0, false>(rest, rest);
+        accumulate<0>(rest);
       }
     }
   }
@@ -519,11 +517,11 @@ struct WaveAttention {
     if constexpr (F == kPair) {
       step_pair<SECOND>(area, alpha, on && ks < 2, on && masked(first_key, 64), fine, visible);
     } else if constexpr (F == kBoth) {
-      if (on && ks == 0) step<OFF, SECOND>(alpha, masked(first_key, 64), visible);
+      if (on && ks == 0) step<OFF, SECOND>(alpha, masked(first_key, 64), fine, visible);
     } else if (on && ks < streams) {
-      if (streams == 1 || ks == 0) step<OFF, SECOND>(alpha, masked(first_key, 32), visible);
+      if (streams == 1 || ks == 0) step<OFF, SECOND>(alpha, masked(first_key, 32), fine, visible);
       if (streams == 1 || ks == 1)
-        step<OFF + 32 * S::kPitch, SECOND>(alpha, masked(first_key + 32, 32), [&](int, int r) { return visible(1, r); });
+        step<OFF + 32 * S::kPitch, SECOND>(alpha, masked(first_key + 32, 32), fine, [&](int, int r) { return visible(1, r); });
     }
   }
 
@@ -663,45 +661,88 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// Joins the parts of one row: part s is row first + s * stride of the partial
-// results.  A wave takes a row, its lanes D / 64 channels each (at D = 32 the
-// lower half, and lanes past D are given nothing to write).
-template <int D>
+// Joins the parts of a row.  WAVES waves of a workgroup share it, every WAVES-th
+// part to each; a lane has D / 64 channels (at D = 32 the upper half of a wave
+// repeats the lower).  A wave reads the references and sums of 64 parts at once, and
+// eight parts' sums are in flight together.
+template <int D, int WAVES>
 struct JoinedRow {
   static constexpr int kPer = D >= 64 ? D / 64 : 1;
   typedef float vec __attribute__((ext_vector_type(kPer)));
+  struct Shared {
+    float m[4], l[4], o[4][64 * kPer];
+  };
   float m = -INFINITY, l = 0.0f, o[kPer] = {};
 
-  __device__ __forceinline__ JoinedRow(const float* part_o, const float* part_ml, int64_t first, int64_t stride,
-                                       int parts) {
-    const int lane = threadIdx.x & 63;
+  // Part s is row first + s * stride of the partial results.
+  __device__ __forceinline__ void add(const float* part_o, const float* part_ml, int64_t first, int64_t stride, int parts) {
+    const int lane = threadIdx.x & 63, wave = WAVES > 1 ? static_cast<int>(threadIdx.x >> 6) % WAVES : 0;
     const float* po = part_o + kPer * (D >= 64 ? lane : lane & 31);
-    for (int s0 = 0; s0 < parts; s0 += 64) {  // references and sums of up to 64 parts at once
+    const int mine = (parts - wave + WAVES - 1) / WAVES;
+    for (int s0 = 0; s0 < mine; s0 += 64) {
+      const int n = min(64, mine - s0);
+      const int64_t from = first + (wave + static_cast<int64_t>(WAVES) * s0) * stride;
       floatx2 ml = {-INFINITY, 0.0f};
-      if (s0 + lane < parts) ml = *reinterpret_cast<const floatx2*>(part_ml + 2 * (first + (s0 + lane) * stride));
+      if (lane < n) ml = *reinterpret_cast<const floatx2*>(part_ml + 2 * (from + WAVES * lane * stride));
+      vec x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const vec*>(po + (from + min(i, n - 1) * WAVES * stride) * D);
       float top = ml.x;
 #pragma unroll
-      for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+      for (int y = 32; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
       const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
       const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
       float sum = ml.y * f;  // 0 of a part that saw nothing
 #pragma unroll
-      for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+      for (int y = 32; y > 0; y >>= 1) sum += __shfl_xor(sum, y);
       l = l * keep + sum;
       m = mn;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) o[i] *= keep;
-      const uint64_t seen = __ballot(ml.x != -INFINITY || ml.y != 0.0f);  // the others wrote no sums
-      const int n = min(64, parts - s0);
-#pragma unroll 4
-      for (int s = 0; s < n; ++s) {
-        const float fs = __shfl(f, s);
-        if (!(seen >> s & 1)) continue;
-        const vec x = *reinterpret_cast<const vec*>(po + (first + (s0 + s) * stride) * D);
+      const uint64_t seen = __ballot(ml.x != -INFINITY || ml.y != 0.0f);  // the others may have written no sums
+      for (int s = 0; s < n; s += 8) {
+        vec next[8];
+        if (s + 8 < n) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) o[i] += x[i] * fs;
+          for (int i = 0; i < 8; ++i)
+            next[i] = *reinterpret_cast<const vec*>(po + (from + min(s + 8 + i, n - 1) * WAVES * stride) * D);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (s + i >= n) break;
+          const float fs = __shfl(f, s + i);
+          const bool use = seen >> (s + i) & 1;
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) o[c] += (use ? x[i][c] : 0.0f) * fs;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = next[i];
       }
     }
+  }
+  // The waves' shares together, in wave 0 of the row (true there).
+  __device__ __forceinline__ bool together(Shared& sh) {
+    if constexpr (WAVES > 1) {
+      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+      if (lane == 0) {
+        sh.m[wave] = m;
+        sh.l[wave] = l;
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) sh.o[wave][kPer * lane + i] = o[i];
+      __syncthreads();
+      if (wave != 0) return false;
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) {
+        const float mn = fmaxf(m, sh.m[w]), ref = mn == -INFINITY ? 0.0f : mn;
+        const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(sh.m[w] - ref);
+        m = mn;
+        l = l * a + sh.l[w] * b;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[i] = o[i] * a + sh.o[w][kPer * lane + i] * b;
+      }
+    }
+    return true;
   }
   template <class E>
   __device__ __forceinline__ void write(typename E::elem* out) const {
@@ -712,5 +753,7 @@ struct JoinedRow {
       if (D >= 64 || lane < D) out[kPer * lane + i] = static_cast<typename E::elem>(o[i] * inv);
   }
 };
+// Rows for which a wave each would leave most of the GPU idle get four.
+constexpr uint64_t kFewRows = 2048;
 
 }  // namespace skv

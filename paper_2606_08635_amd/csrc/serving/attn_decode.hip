@@ -5,8 +5,9 @@
 //   prefix  all B Lq G rows of a KV head (128 per workgroup) against the shared
 //           positions, so a key is loaded once per row block and not per request;
 //   rest    the Lq G rows of one request against its own positions.
-// Ranges are cut into parts that fill the GPU; a second launch joins a row's
-// parts.  A workgroup turns its range into a list of cache rows in shared memory
+// The prefix is cut into equal parts and the requests' rests, one behind the other,
+// into equal slices, so that the work is even whatever the lengths; a second launch
+// joins a row's parts.  A workgroup turns its range into a list of cache rows in shared memory
 // first (up to kList positions at a time): positions past the request's end and
 // DROP tokens are left out, so the tiles that follow hold kept tokens only and a
 // dropped token costs neither bandwidth nor a product.  The tiles gather the
@@ -26,59 +27,80 @@ struct Lists {
   uint32_t scan[THREADS / 64];
 };
 
-// The kept positions of [p0, p1), p1 - p0 <= kList, in order.  The caller's
-// barrier before the call has ended every use of the previous list.
+// The next positions' pages and tiers: loaded while the tiles before them are
+// multiplied, turned into a list afterwards.
 template <int THREADS>
-__device__ __forceinline__ int build_list(const DecodeArgs& a, Lists<THREADS>& s, const int32_t* table, const uint8_t* tier,
-                                          int p0, int p1) {
-  constexpr int kPer = kList / THREADS;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t row[kPer], n = 0;
-  const int first = p0 + kPer * static_cast<int>(threadIdx.x);
-  bool bad = false;
+struct Upcoming {
+  static constexpr int kPer = kList / THREADS;
+  int32_t page[kPer];
+  uint32_t tier[kPer];
+  int first;
+
+  // positions [p0, p1), p1 - p0 <= kList
+  __device__ __forceinline__ void load(const DecodeArgs& a, const int32_t* table, const uint8_t* tiers, int p0, int p1) {
+    first = p0 + kPer * static_cast<int>(threadIdx.x);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int p = first + i;
-    row[i] = -1;
-    if (p >= p1) continue;
-    const int at = static_cast<int>(a.by_block.div(static_cast<uint32_t>(p)));
-    const int page = table[at];
-    const bool kept = tier == nullptr || p >= a.tier_len || tier[p] != kDROP;
-    if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(a.num_blocks)) bad = true;
-    else if (kept) row[i] = page * a.block_size + (p - at * a.block_size);
-    n += row[i] >= 0;
-  }
-  if (bad && a.status != nullptr) *a.status = SKV_ERR_FORMAT;
-  const uint32_t inc = wave_inclusive_scan(static_cast<uint32_t>(n));
-  if (lane == 63) s.scan[wave] = inc;
-  __syncthreads();
-  int to = static_cast<int>(inc) - n, count = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w < wave) to += static_cast<int>(s.scan[w]);
-    count += static_cast<int>(s.scan[w]);
-  }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i)
-    if (row[i] >= 0) {
-      s.rows[to] = row[i];
-      s.pos[to] = first + i;
-      ++to;
+    for (int i = 0; i < kPer; ++i) {
+      const int p = first + i;
+      page[i] = 0;
+      tier[i] = kDROP;
+      if (p >= p1) continue;
+      page[i] = table[a.by_block.div(static_cast<uint32_t>(p))];
+      tier[i] = kFP16;
+      if (tiers != nullptr && p < a.tier_len) tier[i] = tiers[p];
     }
-  const int past = count + static_cast<int>(threadIdx.x);
-  if (past < (count + 63) / 64 * 64) s.pos[past] = INT32_MAX;
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(count);
-}
+  }
+  // Lists the kept positions in order and returns how many; before the call a
+  // barrier has ended every use of the previous list.
+  __device__ __forceinline__ int list(const DecodeArgs& a, Lists<THREADS>& s) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int32_t row[kPer], n = 0;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = first + i;
+      const bool inside = static_cast<uint32_t>(page[i]) < static_cast<uint32_t>(a.num_blocks);
+      bad |= !inside;
+      row[i] = -1;
+      if (inside && tier[i] != kDROP)
+        row[i] = page[i] * a.block_size + (p - static_cast<int>(a.by_block.div(static_cast<uint32_t>(p))) * a.block_size);
+      n += row[i] >= 0;
+    }
+    if (bad && a.status != nullptr) *a.status = SKV_ERR_FORMAT;
+    const uint32_t inc = wave_inclusive_scan(static_cast<uint32_t>(n));
+    if (lane == 63) s.scan[wave] = inc;
+    __syncthreads();
+    int to = static_cast<int>(inc) - n, count = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) to += static_cast<int>(s.scan[w]);
+      count += static_cast<int>(s.scan[w]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (row[i] >= 0) {
+        s.rows[to] = row[i];
+        s.pos[to] = first + i;
+        ++to;
+      }
+    const int past = count + static_cast<int>(threadIdx.x);
+    if (past < (count + 63) / 64 * 64) s.pos[past] = INT32_MAX;
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(count);
+  }
+};
 
 // Rows [row0, row0 + rows) of the launch's B Lq G (row = (request * Lq + query) *
-// G + head of the group) against positions [p0, p1) of `table`.
+// G + head of the group) against positions [p0, p1) of `table`.  part_row: the
+// first row's place in the partial results; -1: results are written at once.
 template <class E, int D, Form F>
 __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, typename WaveAttention<E, D, F>::AreaType& area,
-                                       Lists<Stage<D>::kThreads>& lists, int h, int row0, int rows, int tiles, const int32_t* table,
-                                       const uint8_t* tier, int p0, int p1, int part, bool only) {
+                                       Lists<Stage<D>::kThreads>& lists, int h, int row0, int rows, int tiles,
+                                       const int32_t* table, const uint8_t* tiers, int p0, int p1, int64_t part_row) {
   typedef Stage<D> S;
   typedef WaveAttention<E, D, F> Wave;
+  Upcoming<S::kThreads> next;
+  next.load(a, table, tiers, p0, min(p1, p0 + kList));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   Wave w;
   w.init(stage, tiles, tiles == 4 ? 1 : 2);
@@ -88,6 +110,7 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
   const uint32_t token = a.by_G.div(row), g = row - token * a.G;
   const uint32_t b = a.by_Lq.div(token), i = token - b * a.Lq;
   const int head = h * a.G + static_cast<int>(g);
+  w.load_q(a.q + b * a.q_request + i * a.q_token + head * a.q_head);
   const int len = min(max(a.lens[b], 0), a.width * a.block_size);
   const int limit = len - a.Lq + static_cast<int>(i);  // the row's last visible position
   int wave_min = limit;
@@ -95,16 +118,16 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
   for (int x = 16; x > 0; x >>= 1) wave_min = min(wave_min, __shfl_xor(wave_min, x));
   wave_min = __builtin_amdgcn_readfirstlane(wave_min);
 
-  w.load_q(a.q + b * a.q_request + i * a.q_token + head * a.q_head);
   const int prow = static_cast<int>(threadIdx.x) / S::kCpr, place = static_cast<int>(threadIdx.x) % S::kCpr;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(stage) + static_cast<uint32_t>(wave * 1024));
   const int64_t cache_row = static_cast<int64_t>(a.H) * D;
   const uint16_t* kbase = a.k + h * D;
   const uint16_t* vbase = a.v + h * D;
   walk_tiles(w, area, [&](auto second) {
+    if (decltype(second)::value) next.load(a, table, tiers, p0, min(p1, p0 + kList));
     for (int q0 = p0; q0 < p1; q0 += kList) {
       const int q1 = min(p1, q0 + kList);
-      const int count = build_list(a, lists, table, tier, q0, q1);
+      const int count = next.list(a, lists);
       const int nt = (count + S::kKeys - 1) / S::kKeys;
       const bool cut = q1 - 1 > wave_min;  // some row ends before the list does
       auto issue = [&](int t, int buffer) {
@@ -124,23 +147,32 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
       };
       auto shown = [&](int key) { return lists.pos[key] <= limit; };
       auto tile = [&](int t, auto offset, auto again) {
-        w.template tile<decltype(offset)::value, decltype(again)::value>(area, a.alpha, t * S::kKeys, active, true, masked,
-                                                                          shown);
+        // (rows of one request are a bandwidth-bound product: two terms cost nothing there)
+        w.template tile<decltype(offset)::value, decltype(again)::value>(area, a.alpha, t * S::kKeys, active, tiles < 4,
+                                                                          masked, shown);
       };
+      w.wait_q();
+      if (q1 < p1) next.load(a, table, tiers, q1, min(p1, q1 + kList));
       walk_once<D, decltype(second)::value>(w, 0, nt, issue, tile);
       if (q1 < p1) __syncthreads();  // the next list
     }
   });
   const bool writes = w.finish(stage, area, active);
   if (!writes || mine >= rows) return;
-  if (only) {
+  if (part_row < 0) {
     w.write_out(a.out + b * a.out_request + i * a.out_token + head * a.out_head, inverse_or_zero(w.l));
     if (a.lse != nullptr && w.writes_sum()) a.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, w.l);
     return;
   }
-  const int64_t at = (static_cast<int64_t>(part) * a.H + h) * (static_cast<int64_t>(a.B) * a.Lq * a.G) + row;
-  if (p0 < p1) w.write_partial(a.part_o + at * D);
-  if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * at) = floatx2{w.m, w.l};
+  w.write_partial(a.part_o + (part_row + mine) * D);
+  if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * (part_row + mine)) = floatx2{w.m, w.l};
+}
+
+// Tokens of request b past the prefix.
+__device__ __forceinline__ int tail_tokens(const DecodeArgs& a, int b) {
+  const int given = a.lens[b], len = min(max(given, 0), a.width * a.block_size);
+  if (given != len && a.status != nullptr) *a.status = SKV_ERR_FORMAT;
+  return max(len - a.prefix, 0);
 }
 
 template <class E, int D>
@@ -149,59 +181,121 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
   __shared__ __align__(1024) uint8_t stage[2 * Stage<D>::kBytes];
   __shared__ typename WaveAttention<E, D, F>::AreaType area;
   __shared__ Lists<Stage<D>::kThreads> lists;
+  __shared__ int32_t ends[kSlicedRequests];  // tiles of the tails up to each request's end
   uint32_t at = blockIdx.x;
   const uint32_t H = static_cast<uint32_t>(a.H);
-  int h, row0, rows, tiles, p0, p1, part;
-  const int32_t* table;
-  const uint8_t* tier;
-  if (at < a.prefix_groups) {
-    h = static_cast<int>(at % H);
+  const int h = static_cast<int>((at < a.prefix_groups ? at : at - a.prefix_groups) % H);
+  const int own = a.Lq * a.G, rows_all = a.B * own;
+  int blk, tiles, b = 0, t = 0, t1 = 1;  // tail: request and tiles of the slice
+  const bool prefix = at < a.prefix_groups;
+  if (prefix) {
     at /= H;
-    const int blk = static_cast<int>(at % static_cast<uint32_t>(a.prefix_blocks));
-    part = static_cast<int>(at / static_cast<uint32_t>(a.prefix_blocks));
+    blk = static_cast<int>(at % static_cast<uint32_t>(a.prefix_blocks));
+    t = static_cast<int>(at / static_cast<uint32_t>(a.prefix_blocks));  // the part
+    t1 = t + 1;
     tiles = a.prefix_tiles;
-    row0 = blk * tiles * 32;
-    rows = min(tiles * 32, a.B * a.Lq * a.G - row0);
-    p0 = part * a.prefix_chunk;
-    p1 = min(a.prefix, p0 + a.prefix_chunk);
-    table = a.tables;
-    tier = a.tiers == nullptr ? nullptr : a.tiers + h * a.tier_head;
   } else {
-    at -= a.prefix_groups;
-    h = static_cast<int>(at % H);
-    at /= H;
-    const int blk = static_cast<int>(at % static_cast<uint32_t>(a.tail_blocks));
+    at = (at - a.prefix_groups) / H;
+    blk = static_cast<int>(at % static_cast<uint32_t>(a.tail_blocks));
     at /= static_cast<uint32_t>(a.tail_blocks);
-    part = static_cast<int>(at % static_cast<uint32_t>(a.tail_parts));
-    const int b = static_cast<int>(at / static_cast<uint32_t>(a.tail_parts));
     tiles = a.tail_tiles;
-    row0 = b * a.Lq * a.G + blk * tiles * 32;
-    rows = min(tiles * 32, a.Lq * a.G - blk * tiles * 32);
-    const int given = a.lens[b], most = a.width * a.block_size, len = min(max(given, 0), most);
-    if (given != len && a.status != nullptr) *a.status = SKV_ERR_FORMAT;
-    // whole tiles to each part
-    const int n = max(len - a.prefix, 0), tilesn = (n + 63) / 64, chunk = (tilesn + a.tail_parts - 1) / a.tail_parts * 64;
-    p0 = a.prefix + min(n, part * chunk);
-    p1 = a.prefix + min(n, part * chunk + chunk);
-    part += a.prefix_parts;
-    table = a.tables + b * a.table_stride;
-    tier = a.tiers == nullptr ? nullptr : a.tiers + b * a.tier_request + h * a.tier_head;
+    if (a.slices == 0) {
+      b = static_cast<int>(at);
+    } else {
+      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x;
+      const int n = me < a.B ? (tail_tokens(a, me) + 63) / 64 : 0;
+      const uint32_t inc = wave_inclusive_scan(static_cast<uint32_t>(n));
+      if (lane == 63) lists.scan[wave] = inc;
+      __syncthreads();
+      int end = static_cast<int>(inc), all = 0;
+#pragma unroll
+      for (int w = 0; w < kSlicedRequests / 64; ++w) {
+        if (w < wave) end += static_cast<int>(lists.scan[w]);
+        all += static_cast<int>(lists.scan[w]);
+      }
+      if (me < kSlicedRequests) ends[me] = end;
+      const int runs = min(a.slices, max(all, 1));  // a tile at least to each: every slice of a request has a part
+      auto start_of = [&](int s) { return static_cast<int>(static_cast<int64_t>(all) * s / runs); };
+      if (blockIdx.x == a.prefix_groups && me < a.B) {  // for the join
+        // the slice of tile x is the last one that starts at or before it
+        auto slice_of = [&](int x) {
+          int s = static_cast<int>(static_cast<int64_t>(x) * runs / all);
+          while (s + 1 < runs && start_of(s + 1) <= x) ++s;
+          return s;
+        };
+        const int s0 = n > 0 ? slice_of(end - n) : -1;
+        a.first_slice[me] = s0;
+        a.part_count[me] = n > 0 ? slice_of(end - 1) - s0 + 1 : 0;
+      }
+      __syncthreads();
+      if (static_cast<int>(at) >= runs) return;
+      t = start_of(static_cast<int>(at));
+      t1 = start_of(static_cast<int>(at) + 1);
+      int hi = a.B - 1;  // the first request that ends behind tile t
+      while (b < hi) {
+        const int mid = (b + hi) >> 1;
+        if (ends[mid] > t) hi = mid;
+        else b = mid + 1;
+      }
+    }
   }
-  const bool only = a.prefix_parts + a.tail_parts == 1;
-  attend<E, D, F>(a, stage, area, lists, h, row0, rows, tiles, table, tier, p0, p1, part, only);
+  const int slice = static_cast<int>(at);
+  while (t < t1) {
+    int row0, rows, p0, p1;
+    int64_t part_row;
+    const int32_t* table = a.tables + b * a.table_stride;
+    const uint8_t* tiers = a.tiers == nullptr ? nullptr : a.tiers + b * a.tier_request + h * a.tier_head;
+    if (prefix) {
+      row0 = blk * tiles * 32;
+      rows = min(tiles * 32, rows_all - row0);
+      p0 = t * a.prefix_chunk;
+      p1 = min(a.prefix, p0 + a.prefix_chunk);
+      part_row = (static_cast<int64_t>(t) * a.H + h) * rows_all + row0;
+      ++t;
+    } else {
+      row0 = b * own + blk * tiles * 32;
+      rows = min(tiles * 32, own - blk * tiles * 32);
+      const int n = tail_tokens(a, b);
+      if (a.slices == 0) {
+        p0 = a.prefix;
+        p1 = a.prefix + n;
+        t = t1;
+      } else {
+        const int begin = b > 0 ? ends[b - 1] : 0, stop = min(t1, ends[b]);
+        p0 = a.prefix + 64 * (t - begin);
+        p1 = a.prefix + min(n, 64 * (stop - begin));
+        t = stop;
+      }
+      part_row = a.direct ? -1
+                          : a.tail_at + (static_cast<int64_t>(a.slices == 0 ? b : slice + b) * a.H + h) * own + blk * tiles * 32;
+    }
+    attend<E, D, F>(a, stage, area, lists, h, row0, rows, tiles, table, tiers, p0, p1, part_row);
+    if (t >= t1) break;
+    __syncthreads();  // the stage and the lists are free
+    do ++b;  // the next request with a tail
+    while (b < a.B - 1 && ends[b] <= t);
+  }
 }
 
-// Joins the parts of each row: one wave per (KV head, row).
-template <class E, int D>
+// Joins the parts of each row: WAVES waves per (KV head, row).
+template <class E, int D, int WAVES>
 __global__ __launch_bounds__(256) void attn_decode_join(const DecodeArgs a) {
-  const int64_t rows = static_cast<int64_t>(a.B) * a.Lq * a.G;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // h * rows + row
+  __shared__ typename JoinedRow<D, WAVES>::Shared shared;
+  const int own = a.Lq * a.G;
+  const int64_t rows = static_cast<int64_t>(a.B) * own;
+  const int64_t at = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) / WAVES;  // h * rows + row
   if (at >= rows * a.H) return;
-  const JoinedRow<D> j(a.part_o, a.part_ml, at, rows * a.H, a.prefix_parts + a.tail_parts);
   const int h = static_cast<int>(at / rows);
   const uint32_t row = static_cast<uint32_t>(at - h * rows);
   const uint32_t token = a.by_G.div(row), g = row - token * a.G;
   const uint32_t b = a.by_Lq.div(token), i = token - b * a.Lq;
+  JoinedRow<D, WAVES> j;
+  j.add(a.part_o, a.part_ml, at, rows * a.H, a.prefix_parts);
+  const int slice = a.slices == 0 ? 0 : a.first_slice[b];
+  const int64_t stride = static_cast<int64_t>(a.H) * own;
+  j.add(a.part_o, a.part_ml, a.tail_at + (static_cast<int64_t>(slice) + b) * stride + static_cast<int64_t>(h) * own + (row - b * own),
+        stride, a.slices == 0 ? 1 : a.part_count[b]);
+  if (!j.together(shared)) return;
   const int head = h * a.G + static_cast<int>(g);
   j.template write<E>(reinterpret_cast<typename E::elem*>(a.out + b * a.out_request + i * a.out_token + head * a.out_head));
   if (a.lse != nullptr && (threadIdx.x & 63) == 0)
@@ -212,9 +306,10 @@ template <class E, int D>
 hipError_t launch(const DecodeArgs& a, hipStream_t stream) {
   attn_decode<E, D><<<a.groups, Stage<D>::kThreads, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.prefix_parts + a.tail_parts == 1) return e;
+  if (e != hipSuccess || a.direct) return e;
   const uint64_t rows = static_cast<uint64_t>(a.B) * a.Lq * a.G * a.H;
-  attn_decode_join<E, D><<<static_cast<uint32_t>((rows + 3) / 4), 256, 0, stream>>>(a);
+  if (rows <= kFewRows) attn_decode_join<E, D, 4><<<static_cast<uint32_t>(rows), 256, 0, stream>>>(a);
+  else attn_decode_join<E, D, 1><<<static_cast<uint32_t>((rows + 3) / 4), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -79,6 +79,7 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
         area, a.alpha, key0, active && key0 <= wave_max, false, [&](int key, int keys) { return key + keys - 1 > wave_min; },
         [&](int key) { return key <= limit; });
   };
+  w.wait_q();
   walk_tiles(w, area, [&](auto second) { walk_once<D, decltype(second)::value>(w, t0, t1, issue, tile); });
   const bool writes = w.finish(stage, area, active);
   if (!writes || row0 + (lane & 31) >= rows) return;  // (both lane-halves of a row stay: write_out pairs them)
@@ -92,19 +93,22 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
   if (r.lse != nullptr && w.writes_sum()) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, w.l);
 }
 
-// Joins the parts of requests with splits > 1: one wave per row.
-template <class E, int D>
+// Joins the parts of a request with splits > 1: WAVES waves per row.
+template <class E, int D, int WAVES>
 __global__ __launch_bounds__(256) void attn_prompt_join(const PromptArgs a, int ri) {
+  __shared__ typename JoinedRow<D, WAVES>::Shared shared;
   const PromptDesc& r = a.r[ri];
   const int rows = r.nq * a.G;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);  // h * rows + row
+  const int64_t at = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) / WAVES;  // h * rows + row
   if (at >= static_cast<int64_t>(rows) * a.H) return;
-  const int lane = threadIdx.x & 63;
   const int h = static_cast<int>(at / rows), row = static_cast<int>(at % rows);
-  const JoinedRow<D> j(a.part_o, a.part_ml, r.rows_at + at, static_cast<int64_t>(rows) * a.H, r.splits);
+  JoinedRow<D, WAVES> j;
+  j.add(a.part_o, a.part_ml, r.rows_at + at, static_cast<int64_t>(rows) * a.H, r.splits);
+  if (!j.together(shared)) return;
   const int token = row / a.G, head = h * a.G + row % a.G;
   j.template write<E>(reinterpret_cast<typename E::elem*>(r.out + token * a.out_token + head * a.out_head));
-  if (r.lse != nullptr && lane == 0) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(j.m, j.l);
+  if (r.lse != nullptr && (threadIdx.x & 63) == 0)
+    r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(j.m, j.l);
 }
 
 template <class E, int D>
@@ -116,7 +120,8 @@ hipError_t launch(const PromptArgs& a, hipStream_t stream) {
   for (int i = 0; i < a.count && e == hipSuccess; ++i) {
     if (a.r[i].splits <= 1) continue;
     const uint64_t rows = static_cast<uint64_t>(a.r[i].nq) * a.G * a.H;
-    attn_prompt_join<E, D><<<static_cast<uint32_t>((rows + 3) / 4), 256, 0, stream>>>(a, i);
+    if (rows <= kFewRows) attn_prompt_join<E, D, 4><<<static_cast<uint32_t>(rows), 256, 0, stream>>>(a, i);
+    else attn_prompt_join<E, D, 1><<<static_cast<uint32_t>((rows + 3) / 4), 256, 0, stream>>>(a, i);
     e = hipGetLastError();
   }
   return e;

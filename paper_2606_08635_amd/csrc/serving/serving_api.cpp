@@ -50,6 +50,9 @@ skv_status check_prompt(const skv_attn_config* c, const skv_attn_request* reqs, 
   return SKV_OK;
 }
 
+// 32-row tiles of a workgroup for this many rows.
+int32_t row_tiles(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
 // How a launch of requests [0, n) (already ordered) runs.
 struct PromptPlan {
   int32_t key_streams, row_tiles;
@@ -64,21 +67,34 @@ int64_t prompt_blocks(const skv_attn_config* c, const skv_attn_request& r, int32
 
 PromptPlan plan_prompt(const skv_attn_config* c, const std::vector<const skv_attn_request*>& reqs) {
   PromptPlan p{1, 4, {}, 0};
+  const int64_t room = c->head_dim >= 256 ? kCus : 2 * kCus;  // workgroups that the GPU holds at once
   auto blocks = [&](int32_t tiles) {
     int64_t n = 0;
     for (const skv_attn_request* r : reqs) n += prompt_blocks(c, *r, 32 * tiles);
     return n;
   };
-  if (blocks(4) < 2 * kCus) {
-    p.key_streams = 2;
-    p.row_tiles = blocks(2) < kCus ? 1 : 2;
+  int32_t most_keys = 0;
+  int64_t most_rows = 0;
+  for (const skv_attn_request* r : reqs) {
+    most_keys = std::max(most_keys, r->num_keys);
+    most_rows = std::max(most_rows, static_cast<int64_t>(r->num_queries) * (c->num_q_heads / c->num_kv_heads));
   }
-  const int64_t all = blocks(p.row_tiles);
+  // Workgroups of 128 rows, the most work per byte staged, where they fill three
+  // quarters of the room or their keys will be split; otherwise of 64 or 32 rows with
+  // two waves per row tile (1000 queries of 16 x 256 on 8 KV heads: 30 us against 40).
+  const bool splits = most_keys > 1024;
+  if (blocks(4) * 4 < room * 3 && !(splits && most_rows >= 128)) {
+    p.key_streams = 2;
+    p.row_tiles = row_tiles(std::min<int64_t>(most_rows, 64));
+  }
+  // Parts of at least 256 keys that fill the room (100 queries of 32 x 128 over 30000
+  // keys: 474 us in one part, 77 in 16); a second launch and its traffic cost about
+  // 10 us, so short keys are left whole.
+  const int64_t all = std::max<int64_t>(1, blocks(p.row_tiles));
   for (const skv_attn_request* r : reqs) {
     const int64_t rows = static_cast<int64_t>(r->num_queries) * c->num_q_heads;
     int64_t s = 1;
-    if (all < kCus) s = std::min<int64_t>(2 * kCus / std::max<int64_t>(all, 1), r->num_keys / 512);
-    s = std::max<int64_t>(1, std::min<int64_t>(s, 64));
+    if (splits && 2 * all <= room) s = std::max<int64_t>(1, std::min<int64_t>({room / all, r->num_keys / 256, 64}));
     p.splits.push_back(static_cast<int32_t>(s));
     if (s > 1) p.rows += static_cast<uint64_t>(rows * s);
   }
@@ -110,33 +126,37 @@ skv_status prompt_launches(const skv_attn_config* c, const skv_attn_request* req
 // How skv_attn_decode cuts its work (the counts, lengths and dimensions of c are
 // valid).
 struct DecodePlan {
-  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, tail_parts, tail_blocks, tail_tiles;
-  uint64_t prefix_groups, groups, part_bytes;
+  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, slices, tail_blocks, tail_tiles;
+  uint64_t prefix_groups, groups, prefix_rows, part_rows, bytes;  // (bytes 0: no parts)
 };
-
-int32_t row_tiles(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
 DecodePlan plan_decode(const skv_decode_config* c) {
   DecodePlan p{};
   const int64_t H = c->num_kv_heads, G = c->num_q_heads / H, own = c->num_queries * G, all = own * c->num_requests;
   const int64_t tail = std::max(0, c->max_len - c->prefix_len);
-  const int64_t want = 2 * kCus;
+  const int64_t room = c->head_dim >= 256 ? kCus : 2 * kCus;  // workgroups that the GPU holds at once
   auto up = [](int64_t x, int64_t to) { return (x + to - 1) / to; };
   p.tail_tiles = row_tiles(own);
   p.tail_blocks = static_cast<int32_t>(up(own, 32 * p.tail_tiles));
-  const int64_t tails = c->num_requests * H * p.tail_blocks;
-  p.tail_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({up(want, tails), up(tail, 128), 256})));
+  // slices where requests are few or long, of 128 tokens at least (as far as max_len says)
+  const int64_t groups = H * p.tail_blocks;
+  const int64_t slices = std::min(std::max<int64_t>(1, room / groups), up(c->num_requests * tail, 128));
+  if (c->num_requests <= kSlicedRequests && tail > 256 && slices > 1) p.slices = static_cast<int32_t>(slices);
   if (c->prefix_len > 0) {
     p.prefix_tiles = row_tiles(all);
     p.prefix_blocks = static_cast<int32_t>(up(all, 32 * p.prefix_tiles));
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({up(want, H * p.prefix_blocks), up(c->prefix_len, 128), 256}));
+    const int64_t parts = std::max<int64_t>(1, std::min(room / (H * p.prefix_blocks), up(c->prefix_len, 128)));
     p.prefix_chunk = static_cast<int32_t>(up(up(c->prefix_len, parts), 64) * 64);
     p.prefix_parts = static_cast<int32_t>(up(c->prefix_len, p.prefix_chunk));
     p.prefix_groups = static_cast<uint64_t>(H * p.prefix_blocks * p.prefix_parts);
+    p.prefix_rows = static_cast<uint64_t>(p.prefix_parts * H * all);
   }
-  p.groups = p.prefix_groups + static_cast<uint64_t>(tails * p.tail_parts);
-  const int64_t parts = p.prefix_parts + p.tail_parts;
-  if (parts > 1) p.part_bytes = static_cast<uint64_t>(parts * H * all) * static_cast<uint64_t>(c->head_dim + 2) * 4u;
+  const int64_t runs = p.slices > 0 ? p.slices : c->num_requests;
+  p.groups = p.prefix_groups + static_cast<uint64_t>(groups * runs);
+  if (p.prefix_parts == 0 && p.slices == 0) return p;
+  const int64_t places = p.slices > 0 ? p.slices + c->num_requests : c->num_requests;
+  p.part_rows = p.prefix_rows + static_cast<uint64_t>(places * H * own);
+  p.bytes = p.part_rows * static_cast<uint64_t>(c->head_dim + 2) * 4u + 8u * static_cast<uint64_t>(c->num_requests);
   return p;
 }
 
@@ -305,7 +325,7 @@ skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* r
 skv_status skv_attn_decode_workspace_size(const skv_decode_config* cfg, uint64_t* bytes) {
   if (bytes == nullptr) return SKV_ERR_INVALID_ARG;
   const skv_status st = check_decode_sizes(cfg);
-  if (st == SKV_OK) *bytes = plan_decode(cfg).part_bytes;
+  if (st == SKV_OK) *bytes = plan_decode(cfg).bytes;
   return st;
 }
 
@@ -330,10 +350,9 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
       !aligned(tables, 4) || (lse != nullptr && !aligned(lse, 4)) || (dev_status != nullptr && !aligned(dev_status, 4)))
     return SKV_ERR_INVALID_ARG;
   const DecodePlan p = plan_decode(cfg);
-  if (p.part_bytes > 0 && !aligned(ws, 16)) return SKV_ERR_INVALID_ARG;
-  if (ws_bytes < p.part_bytes || p.groups > kMaxGridThreads / 256) return SKV_ERR_CAPACITY;
+  if (p.bytes > 0 && !aligned(ws, 16)) return SKV_ERR_INVALID_ARG;
+  if (ws_bytes < p.bytes || p.groups > kMaxGridThreads / 256) return SKV_ERR_CAPACITY;
   const int32_t H = c.num_kv_heads, G = c.num_q_heads / H;
-  const uint64_t part_rows = static_cast<uint64_t>(p.prefix_parts + p.tail_parts) * c.num_requests * c.num_queries * c.num_q_heads;
   DecodeArgs a;
   std::memset(&a, 0, sizeof(a));
   a.q = static_cast<const uint16_t*>(q);
@@ -346,7 +365,13 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   a.tiers = tiers;
   a.status = dev_status;
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = p.part_bytes > 0 ? a.part_o + part_rows * static_cast<uint64_t>(c.head_dim) : nullptr;
+  a.direct = p.bytes == 0;
+  if (!a.direct) {
+    a.part_ml = a.part_o + p.part_rows * static_cast<uint64_t>(c.head_dim);
+    a.first_slice = reinterpret_cast<int32_t*>(a.part_ml + 2 * p.part_rows);
+    a.part_count = a.first_slice + c.num_requests;
+  }
+  a.tail_at = static_cast<int64_t>(p.prefix_rows);
   a.q_request = c.q_request_stride;
   a.q_token = c.q_token_stride;
   a.q_head = c.q_head_stride;
@@ -369,7 +394,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   a.prefix_blocks = p.prefix_blocks;
   a.prefix_tiles = p.prefix_tiles;
   a.prefix_chunk = p.prefix_chunk;
-  a.tail_parts = p.tail_parts;
+  a.slices = p.slices;
   a.tail_blocks = p.tail_blocks;
   a.tail_tiles = p.tail_tiles;
   a.prefix_groups = static_cast<uint32_t>(p.prefix_groups);
