@@ -138,19 +138,29 @@ DecodePlan plan_decode(const skv_decode_config* c) {
   auto up = [](int64_t x, int64_t to) { return (x + to - 1) / to; };
   p.tail_tiles = row_tiles(own);
   p.tail_blocks = static_cast<int32_t>(up(own, 32 * p.tail_tiles));
-  // slices where requests are few or long, of 128 tokens at least (as far as max_len says)
-  const int64_t groups = H * p.tail_blocks;
-  const int64_t slices = std::min(std::max<int64_t>(1, room / groups), up(c->num_requests * tail, 128));
-  if (c->num_requests <= kSlicedRequests && tail > 256 && slices > 1) p.slices = static_cast<int32_t>(slices);
+  // The prefix gets half the room (a quarter at D = 256, where a compute unit holds one
+  // workgroup), in parts of at least 128 tokens: more parts are more partial results
+  // to write and join (64 requests behind 16384 tokens of 8 x 128: 51 us with 512
+  // workgroups, 41 with 256, 47 with 128).
   if (c->prefix_len > 0) {
     p.prefix_tiles = row_tiles(all);
     p.prefix_blocks = static_cast<int32_t>(up(all, 32 * p.prefix_tiles));
-    const int64_t parts = std::max<int64_t>(1, std::min(room / (H * p.prefix_blocks), up(c->prefix_len, 128)));
+    const int64_t share = c->head_dim >= 256 ? room / 4 : room / 2;
+    const int64_t parts = std::max<int64_t>(1, std::min(share / (H * p.prefix_blocks), up(c->prefix_len, 128)));
     p.prefix_chunk = static_cast<int32_t>(up(up(c->prefix_len, parts), 64) * 64);
     p.prefix_parts = static_cast<int32_t>(up(c->prefix_len, p.prefix_chunk));
     p.prefix_groups = static_cast<uint64_t>(H * p.prefix_blocks * p.prefix_parts);
     p.prefix_rows = static_cast<uint64_t>(p.prefix_parts * H * all);
   }
+  // The tails in slices that fill the rest of the room, of 128 tokens at least (as far
+  // as max_len says), unless the requests fill it as they are and are short: a
+  // slice's further requests cost it about 5 us each (64 requests of up to 400 tokens:
+  // 14 us whole, 36 in slices), uneven lengths cost more from 2048 tokens on.
+  const int64_t groups = H * p.tail_blocks;
+  const int64_t left = std::max<int64_t>(1, room - static_cast<int64_t>(p.prefix_groups));
+  const int64_t slices = std::min(std::max<int64_t>(1, left / groups), up(c->num_requests * tail, 128));
+  const bool whole = tail <= 256 || (tail < 2048 && c->num_requests * groups * 4 >= left * 3);
+  if (c->num_requests <= kSlicedRequests && !whole && slices > 1) p.slices = static_cast<int32_t>(slices);
   const int64_t runs = p.slices > 0 ? p.slices : c->num_requests;
   p.groups = p.prefix_groups + static_cast<uint64_t>(groups * runs);
   if (p.prefix_parts == 0 && p.slices == 0) return p;
