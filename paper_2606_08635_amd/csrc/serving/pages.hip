@@ -138,14 +138,15 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan(const PageArgs a) {
   } else if (a.op == kPagesFork && a.checked) {
     for (int c = tid; c < a.rows; c += kPlanThreads) bad |= a.ws_bad[c] != 0;
   } else if (a.op == kPagesFork) {  // small tables: looked over here
-    for (int c = wave; c < a.rows; c += kPlanWaves) {
-      const int src = source_of(a, c);
-      if (static_cast<uint32_t>(src) >= static_cast<uint32_t>(a.sources) || !length_ok(a, a.lens[src])) {
-        bad |= 1;
-        continue;
-      }
-      const int pages = pages_of(a.lens[src], a.by_block, a.block_size);
-      for (int j = lane; j < pages; j += 64) bad |= !held(a, a.tables[static_cast<int64_t>(src) * a.width + j]);
+    const uint32_t entries = static_cast<uint32_t>(a.rows) * static_cast<uint32_t>(max(1, a.width));
+#pragma unroll 4
+    for (uint32_t e = tid; e < entries; e += kPlanThreads) {
+      const uint32_t c = a.by_width.div(e), j = e - c * static_cast<uint32_t>(max(1, a.width));
+      const int src = source_of(a, static_cast<int>(c));
+      const bool there = static_cast<uint32_t>(src) < static_cast<uint32_t>(a.sources);
+      const int n = there ? a.lens[src] : -1;
+      if (!length_ok(a, n)) bad |= 1;
+      else if (j < static_cast<uint32_t>(pages_of(n, a.by_block, a.block_size))) bad |= !held(a, a.tables[static_cast<int64_t>(src) * a.width + j]);
     }
   } else {
     for (int c = tid; c < a.rows; c += kPlanThreads) bad |= !length_ok(a, a.lens[c]) || !length_ok(a, a.new_lens[c]);
@@ -347,27 +348,40 @@ __global__ __launch_bounds__(256) void pages_apply(const PageArgs a) {
 
 // Releases tables: every page's count goes down by one for each entry that holds
 // it.  An entry out of range, or one more than the count has, is passed over.
-__global__ __launch_bounds__(256) void pages_free(const PageArgs a, int alone) {
+// alone: the launch is this workgroup, which clears the status itself.  Four
+// entries of a thread are in flight together.
+__global__ __launch_bounds__(kPlanThreads) void pages_free(const PageArgs a, int alone) {
   if (alone) {
     if (threadIdx.x == 0) *a.status = SKV_OK;
     __syncthreads();
   }
-  const int64_t all = static_cast<int64_t>(a.rows) * a.width;
+  const uint32_t all = static_cast<uint32_t>(a.rows) * static_cast<uint32_t>(a.width), step = gridDim.x * kPlanThreads;
   bool bad = false;
-  for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < all; e += static_cast<int64_t>(gridDim.x) * 256) {
-    const int b = static_cast<int>(e / a.width), j = static_cast<int>(e % a.width);
-    const int n = a.lens[b];
-    if (!length_ok(a, n)) {
-      bad = true;
-      continue;
+  for (uint64_t e0 = blockIdx.x * kPlanThreads + threadIdx.x; e0 < all; e0 += 4 * static_cast<uint64_t>(step)) {
+    int n[4], page[4];
+    uint32_t j[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t e = e0 + static_cast<uint64_t>(i) * step;
+      n[i] = 0;
+      if (e >= all) continue;
+      const uint32_t b = a.by_width.div(static_cast<uint32_t>(e));
+      j[i] = static_cast<uint32_t>(e) - b * static_cast<uint32_t>(a.width);
+      n[i] = a.lens[b];
+      page[i] = a.tables[e];
     }
-    if (j >= pages_of(n, a.by_block, a.block_size)) continue;
-    const int page = a.tables[e];
-    if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(a.num_blocks)) {
-      bad = true;
-    } else if (atomicSub(a.refs + page, 1) <= 0) {
-      atomicAdd(a.refs + page, 1);
-      bad = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (!length_ok(a, n[i])) {
+        bad = true;
+      } else if (n[i] > 0 && j[i] < static_cast<uint32_t>(pages_of(n[i], a.by_block, a.block_size))) {
+        if (static_cast<uint32_t>(page[i]) >= static_cast<uint32_t>(a.num_blocks)) {
+          bad = true;
+        } else if (atomicSub(a.refs + page[i], 1) <= 0) {
+          atomicAdd(a.refs + page[i], 1);
+          bad = true;
+        }
+      }
     }
   }
   if (bad) *a.status = SKV_ERR_FORMAT;
@@ -385,27 +399,29 @@ __global__ __launch_bounds__(kPlanThreads) void pages_copy_check(const PageCopyA
   if (threadIdx.x == 0) *a.status = any ? SKV_ERR_FORMAT : SKV_OK;
 }
 
-// grid: (pair, plane, piece of a page); a workgroup copies one piece of 32 KB.
-constexpr int kPiece = 32768;
+// Units of work: (pair, plane, 32 KB piece of a page); a workgroup copies four, one
+// after the other, eight 16-byte loads per thread in flight.
+constexpr int kPiece = 32768, kUnits = 4;
 __global__ __launch_bounds__(256) void pages_copy(const PageCopyArgs a, uint32_t first) {
   if (*a.status != SKV_OK) return;
-  uint32_t at = first + blockIdx.x;
-  const uint32_t piece = at % a.pieces;
-  at /= a.pieces;
-  const uint32_t plane = at % a.planes, pair = at / a.planes;
-  const int64_t from = static_cast<int64_t>(plane >> 1) * a.src_plane_bytes + a.src_pages[pair] * a.page_bytes;
-  const int64_t to = static_cast<int64_t>(plane >> 1) * a.dst_plane_bytes + a.dst_pages[pair] * a.page_bytes;
-  const uint8_t* src = (plane & 1 ? a.src_v : a.src_k) + from;
-  uint8_t* dst = (plane & 1 ? a.dst_v : a.dst_k) + to;
-  const int64_t end = min(a.page_bytes, static_cast<int64_t>(piece + 1) * kPiece);
-  const int64_t u0 = static_cast<int64_t>(piece) * kPiece + 16 * static_cast<int>(threadIdx.x);
-  u32x4 x[kPiece / 4096];
+  const uint64_t u0 = static_cast<uint64_t>(first + blockIdx.x) * kUnits;
+  for (uint64_t unit = u0; unit < min(u0 + kUnits, a.units); ++unit) {
+    const uint32_t at = static_cast<uint32_t>(unit / a.pieces), piece = static_cast<uint32_t>(unit % a.pieces);
+    const uint32_t plane = at % a.planes, pair = at / a.planes;
+    const int64_t from = static_cast<int64_t>(plane >> 1) * a.src_plane_bytes + a.src_pages[pair] * a.page_bytes;
+    const int64_t to = static_cast<int64_t>(plane >> 1) * a.dst_plane_bytes + a.dst_pages[pair] * a.page_bytes;
+    const uint8_t* src = (plane & 1 ? a.src_v : a.src_k) + from;
+    uint8_t* dst = (plane & 1 ? a.dst_v : a.dst_k) + to;
+    const int64_t end = min(a.page_bytes, static_cast<int64_t>(piece + 1) * kPiece);
+    const int64_t b0 = static_cast<int64_t>(piece) * kPiece + 16 * static_cast<int>(threadIdx.x);
+    u32x4 x[kPiece / 4096];
 #pragma unroll
-  for (int i = 0; i < kPiece / 4096; ++i)
-    if (u0 + 4096 * i < end) x[i] = ld_nt16(src + u0 + 4096 * i);
+    for (int i = 0; i < kPiece / 4096; ++i)
+      if (b0 + 4096 * i < end) x[i] = ld_nt16(src + b0 + 4096 * i);
 #pragma unroll
-  for (int i = 0; i < kPiece / 4096; ++i)
-    if (u0 + 4096 * i < end) st_nt16(dst + u0 + 4096 * i, x[i]);
+    for (int i = 0; i < kPiece / 4096; ++i)
+      if (b0 + 4096 * i < end) st_nt16(dst + b0 + 4096 * i, x[i]);
+  }
 }
 
 }  // namespace
@@ -428,24 +444,26 @@ hipError_t launch_pages(const PageArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_pages_free(const PageArgs& a, hipStream_t stream) {
-  // one workgroup clears the status itself; more need it cleared before any of them starts
+  // one workgroup clears the status itself (2000 entries: 3 us); more need it cleared
+  // before any of them starts
   const uint64_t all = static_cast<uint64_t>(a.rows) * a.width;
-  const uint32_t groups = all <= 4096 ? 1 : static_cast<uint32_t>(std::min<uint64_t>((all + 1023) / 1024, 1024));
+  const uint32_t groups = all <= 8 * kPlanThreads ? 1 : static_cast<uint32_t>(std::min<uint64_t>((all + 4095) / 4096, 256));
   if (groups > 1) {
     pages_clear_status<<<1, 1, 0, stream>>>(a.status);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  pages_free<<<groups, 256, 0, stream>>>(a, groups == 1);
+  pages_free<<<groups, kPlanThreads, 0, stream>>>(a, groups == 1);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_copy(PageCopyArgs a, hipStream_t stream) {
   a.pieces = static_cast<uint32_t>((a.page_bytes + kPiece - 1) / kPiece);
+  a.units = static_cast<uint64_t>(a.count) * a.planes * a.pieces;
   pages_copy_check<<<1, kPlanThreads, 0, stream>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_pieces(static_cast<uint64_t>(a.count) * a.planes * a.pieces, 256,
+  return launch_pieces((a.units + kUnits - 1) / kUnits, 256,
                        [&](uint32_t first, uint32_t blocks) { pages_copy<<<blocks, 256, 0, stream>>>(a, first); });
 }
 

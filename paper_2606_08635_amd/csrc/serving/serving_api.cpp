@@ -231,6 +231,7 @@ PageArgs page_args(const skv_page_pool* p, const int32_t* tables, int32_t width,
   a.plane_groups = 1;
   a.by_block = make_divider(static_cast<uint32_t>(p->block_size));
   a.by_units = make_divider(static_cast<uint32_t>(p->row_bytes / 16));
+  a.by_width = make_divider(static_cast<uint32_t>(std::max(1, width)));
   return a;
 }
 
@@ -517,7 +518,7 @@ skv_status skv_pages_copy(const skv_page_pool* src, const skv_page_pool* dst, co
   a.src_blocks = src->num_blocks;
   a.dst_blocks = dst->num_blocks;
   a.planes = 2u * static_cast<uint32_t>(src->num_layers);
-  // workgroups of a launch sequence are numbered in 32 bits
+  // units of 32 KB, numbered in 32 bits
   if (static_cast<uint64_t>(count) * a.planes > UINT32_MAX / static_cast<uint64_t>((a.page_bytes + 32767) / 32768))
     return SKV_ERR_CAPACITY;
   return launch_pages_copy(a, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;

@@ -107,7 +107,7 @@ struct PageArgs {
   int32_t op, rows, sources, width, out_width, num_blocks, block_size, num_layers, tier_len;
   int32_t chunks, plane_groups, checked;
   uint32_t copy_groups;
-  Divider by_block, by_units;
+  Divider by_block, by_units, by_width;
 };
 hipError_t launch_pages(const PageArgs& a, hipStream_t stream);
 hipError_t launch_pages_free(const PageArgs& a, hipStream_t stream);
@@ -123,6 +123,7 @@ struct PageCopyArgs {
   int64_t page_bytes, src_plane_bytes, dst_plane_bytes;
   int32_t count, src_blocks, dst_blocks;
   uint32_t planes, pieces;
+  uint64_t units;
 };
 hipError_t launch_pages_copy(PageCopyArgs a, hipStream_t stream);
 

@@ -9,6 +9,7 @@ been built, the first call raises.
 """
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -69,34 +70,6 @@ class GroupSpec(ctypes.Structure):
                 ("budgets", ctypes.POINTER(ctypes.c_float))]
 
 
-class AttnConfig(ctypes.Structure):
-    _fields_ = [("dtype", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
-                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
-                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
-
-
-class AttnRequest(ctypes.Structure):
-    _fields_ = [("num_queries", ctypes.c_int32), ("num_keys", ctypes.c_int32), ("q", ctypes.c_void_p),
-                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
-                ("kv_token_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64)]
-
-
-class DecodeConfig(ctypes.Structure):
-    _fields_ = ([(name, ctypes.c_int32) for name in (
-        "dtype", "num_requests", "num_queries", "num_q_heads", "num_kv_heads", "head_dim", "num_blocks", "block_size",
-        "table_width", "max_len", "prefix_len", "tier_len")] + [("scale", ctypes.c_float)] +
-        [(name, ctypes.c_int64) for name in (
-            "q_request_stride", "q_token_stride", "q_head_stride", "out_request_stride", "out_token_stride",
-            "out_head_stride", "table_stride", "tier_request_stride", "tier_head_stride")])
-
-
-class PagePool(ctypes.Structure):
-    _fields_ = [("num_layers", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32),
-                ("row_bytes", ctypes.c_int32), ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
-                ("refs", ctypes.c_void_p)]
-
-
 class Plan(ctypes.Structure):
     _fields_ = [("n_sink", ctypes.c_int32), ("n_fp16", ctypes.c_int32),
                 ("n_int8", ctypes.c_int32), ("n_int4", ctypes.c_int32),
@@ -147,17 +120,17 @@ def lib():
             "skv_batch_workspace_size": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, P(u64)]),
             "skv_score_batch": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, vp, vp]),
             "skv_assign_batch": (ctypes.c_int, [cfgp, P(ScoreRequest), i32, vp, vp]),
-            "skv_attn_prompt_workspace_size": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, P(u64)]),
-            "skv_attn_decode_workspace_size": (ctypes.c_int, [P(DecodeConfig), P(u64)]),
-            "skv_attn_decode": (ctypes.c_int, [P(DecodeConfig)] + [vp] * 10 + [u64, vp]),
+            "skv_attn_prompt_workspace_size": (ctypes.c_int, [vp, vp, i32, P(u64)]),
+            "skv_attn_decode_workspace_size": (ctypes.c_int, [vp, P(u64)]),
+            "skv_attn_decode": (ctypes.c_int, [vp] + [vp] * 10 + [u64, vp]),
             "skv_pages_workspace_size": (ctypes.c_int, [i32, i32, i32, P(u64)]),
-            "skv_pages_reserve": (ctypes.c_int, [P(PagePool), vp, i32, vp, vp, i32, vp, vp, u64, vp]),
-            "skv_pages_fork": (ctypes.c_int, [P(PagePool), vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, u64, vp]),
-            "skv_pages_compact": (ctypes.c_int, [P(PagePool), vp, i32, vp, i32, vp, i32, ctypes.c_int64, vp, i32, vp,
+            "skv_pages_reserve": (ctypes.c_int, [vp, vp, i32, vp, vp, i32, vp, vp, u64, vp]),
+            "skv_pages_fork": (ctypes.c_int, [vp, vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, u64, vp]),
+            "skv_pages_compact": (ctypes.c_int, [vp, vp, i32, vp, i32, vp, i32, ctypes.c_int64, vp, i32, vp,
                                                  vp, vp, u64, vp]),
-            "skv_pages_free": (ctypes.c_int, [P(PagePool), vp, i32, vp, i32, vp, vp]),
-            "skv_pages_copy": (ctypes.c_int, [P(PagePool), P(PagePool), vp, vp, i32, vp, vp]),
-            "skv_attn_prompt": (ctypes.c_int, [P(AttnConfig), P(AttnRequest), i32, vp, u64, vp]),
+            "skv_pages_free": (ctypes.c_int, [vp, vp, i32, vp, i32, vp, vp]),
+            "skv_pages_copy": (ctypes.c_int, [vp, vp, vp, vp, i32, vp, vp]),
+            "skv_attn_prompt": (ctypes.c_int, [vp, vp, i32, vp, u64, vp]),
         }
         for name, (res, args) in sigs.items():
             fn = getattr(L, name)
@@ -542,27 +515,62 @@ def unpack_batch(cfg: Config, payloads, token_counts, block_tables, k_cache: tor
                                   layer_begin, lc, _stream(stream)), "skv_unpack_batch")
 
 
+# The structures of the attention and page calls, packed at once: building a ctypes
+# structure field by field takes several times as long as the call (a small prompt's
+# call 11 -> 6 us).
 _ATTN_TYPES = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
+_ATTN_CONFIG = struct.Struct("@5if4q")      # skv_attn_config
+_ATTN_REQUEST = struct.Struct("@2i5P2q")    # skv_attn_request
+_DECODE_CONFIG = struct.Struct("@12if9q")   # skv_decode_config
+_PAGE_POOL = struct.Struct("@4i3P")         # skv_page_pool
 
 
-def _rows(t: Optional[torch.Tensor], like: torch.Tensor, shape, name: str) -> int:
-    """Device pointer of a tensor of `like`'s dtype and device and the given shape (None: any size), its last axis contiguous."""
+def _stream_on(device: int, stream) -> int:
+    """The raw stream of a call on tensors of `device`, which must be the current
+    one: the library launches there."""
+    if device != torch.cuda.current_device() or (stream is not None and stream.device_index != device):
+        raise ValueError("the tensors (and the stream) must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _strided(t: Optional[torch.Tensor], dtype, device: int, shape, name: str):
+    """Device pointer and strides of a tensor of this dtype, device and shape
+    whose last axis is contiguous."""
     if t is None:
         raise ValueError(f"{name} is required")
-    if not t.is_cuda or t.device != like.device:
-        raise ValueError(f"{name} must be a device tensor on q's device")
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)):
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be a device tensor, all of them on one device")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    if t.numel() and t.stride(-1) != 1:
+    st = t.stride()
+    if st[-1] != 1 and t.numel():
         raise ValueError(f"{name}'s last axis must be contiguous")
+    return t.data_ptr(), st
+
+
+def _flat(t: Optional[torch.Tensor], dtype, device: int, numel: int, name: str) -> int:
+    """Device pointer of a contiguous tensor on `device` holding at least `numel`
+    elements of `dtype`."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be a device tensor, all of them on one device")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < numel:
+        raise ValueError(f"{name} holds {t.numel()} elements, needs {numel}")
     return t.data_ptr()
 
 
-def _stride(t: torch.Tensor, axis: int) -> int:
-    """Stride of an axis; of one of a single place (torch gives any number there) the one that packing would give."""
-    return t.stride(axis) if t.shape[axis] > 1 else t.shape[-1]
+def _steps(strides, shape):
+    """Strides with those of single-place axes (torch gives any number there) as packing would have them."""
+    if 1 in shape or 0 in shape:
+        return tuple(s if n > 1 else shape[-1] for s, n in zip(strides, shape))
+    return strides
 
 
 def attn_prompt_workspace_size(q_lens, kv_lens, num_q_heads: int, num_kv_heads: int, head_dim: int,
@@ -571,13 +579,10 @@ def attn_prompt_workspace_size(q_lens, kv_lens, num_q_heads: int, num_kv_heads: 
     count = len(q_lens)
     if len(kv_lens) != count:
         raise ValueError("q_lens and kv_lens differ in length")
-    cfg = AttnConfig(DTYPE_F16, num_q_heads, num_kv_heads, head_dim, int(causal), 1.0, 0, 0, 0, 0)
-    reqs = (AttnRequest * count)()
-    for r, nq, nk in zip(reqs, q_lens, kv_lens):
-        r.num_queries, r.num_keys = nq, nk
+    cfg = _ATTN_CONFIG.pack(DTYPE_F16, num_q_heads, num_kv_heads, head_dim, bool(causal), 1.0, 0, 0, 0, 0)
+    reqs = b"".join(_ATTN_REQUEST.pack(nq, nk, 0, 0, 0, 0, 0, 0, 0) for nq, nk in zip(q_lens, kv_lens))
     out = ctypes.c_uint64()
-    _check(lib().skv_attn_prompt_workspace_size(ctypes.byref(cfg), reqs, count, ctypes.byref(out)),
-           "skv_attn_prompt_workspace_size")
+    _check(lib().skv_attn_prompt_workspace_size(cfg, reqs, count, ctypes.byref(out)), "skv_attn_prompt_workspace_size")
     return out.value
 
 
@@ -588,71 +593,76 @@ def attn_prompt(q: torch.Tensor, k, v, out: torch.Tensor, q_lens=None, kv_lens=N
     or bfloat16, any token and head strides), sequence after sequence.  k, v:
     packed the same way, [sum(kv_lens)][H][d], or a list with each sequence's
     [H][n][d] (a layer of the codec's K and V).  q_lens defaults to one
-    sequence, kv_lens to q_lens (packed) or the lists' lengths; causal query i
-    sees keys j <= i + n_keys - n_queries.  scale defaults to 1/sqrt(d).  lse:
-    float32 [sum(q_lens)][Hq], written when given.  ws:
-    attn_prompt_workspace_size bytes, or None (no splitting of the keys)."""
-    if q.dtype not in _ATTN_TYPES:
-        raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
+    sequence, kv_lens to the lists' lengths, or (packed) to one sequence of all
+    keys, else to q_lens; causal query i sees keys j <= i + n_keys - n_queries.
+    scale defaults to 1/sqrt(d).  lse: float32 [sum(q_lens)][Hq], written when
+    given.  ws: attn_prompt_workspace_size bytes, or None (no splitting of the
+    keys)."""
+    dtype, device = q.dtype, q.get_device()
+    if dtype not in _ATTN_TYPES:
+        raise TypeError(f"q must be float16 or bfloat16, got {dtype}")
     if q.dim() != 3:
         raise ValueError("q must be [tokens][heads][d]")
-    total, Hq, d = q.shape
+    shape = q.shape
+    total, Hq, d = shape
     lists = isinstance(k, (list, tuple))
     if lists != isinstance(v, (list, tuple)) or (lists and len(k) != len(v)):
         raise ValueError("k and v must both be packed tensors or lists of one length")
-    q_lens = [total] if q_lens is None else [int(n) for n in q_lens]
-    count = len(q_lens)
     if kv_lens is None:
-        kv_lens = [x.shape[1] for x in k] if lists else q_lens
-    kv_lens = [int(n) for n in kv_lens]
+        kv_lens = [x.shape[1] for x in k] if lists else [k.shape[0]] if q_lens is None else q_lens
+    if q_lens is None:
+        q_lens = [total]
+    count = len(q_lens)
     if len(kv_lens) != count or (lists and len(k) != count):
         raise ValueError("q_lens, kv_lens and the lists of k and v differ in length")
     if min(q_lens, default=0) < 0 or min(kv_lens, default=0) < 0 or sum(q_lens) != total:
         raise ValueError("q_lens must be non-negative and add up to q's tokens")
-    qp, op = _rows(q, q, q.shape, "q"), _rows(out, q, q.shape, "out")
-    lp = None if lse is None else _dev(lse, torch.float32, total * Hq, "lse")
-    H = (k[0].shape[0] if count else 1) if lists else k.shape[1]
-    cfg = AttnConfig(_ATTN_TYPES[q.dtype], Hq, H, d, int(causal), d ** -0.5 if scale is None else scale,
-                     _stride(q, 0), _stride(q, 1), _stride(out, 0), _stride(out, 1))
-    if not lists:
-        if sum(kv_lens) != k.shape[0]:
-            raise ValueError("kv_lens must add up to k's tokens")
-        kp, vp = _rows(k, q, (sum(kv_lens), H, d), "k"), _rows(v, q, k.shape, "v")
-        ks, hs = _stride(k, 0), _stride(k, 1)
-        if (_stride(v, 0), _stride(v, 1)) != (ks, hs):
-            raise ValueError("k and v must have the same strides")
-    reqs = (AttnRequest * count)()
-    qo = oo = lo = ko = 0
-    for i in range(count):
-        r, nq, nk = reqs[i], q_lens[i], kv_lens[i]
-        r.num_queries, r.num_keys = nq, nk
-        r.q, r.out = qp + qo, op + oo
-        if lp is not None:
-            r.lse = lp + lo
-        if lists:
-            r.k, r.v = _rows(k[i], q, (H, nk, d), "k"), _rows(v[i], q, (H, nk, d), "v")
-            r.kv_token_stride, r.kv_head_stride = _stride(k[i], 1), _stride(k[i], 0)
-            if nk and (_stride(v[i], 1), _stride(v[i], 0)) != (r.kv_token_stride, r.kv_head_stride):
+    qp, qs = _strided(q, dtype, device, shape, "q")
+    op, os_ = _strided(out, dtype, device, shape, "out")
+    qs, os_ = _steps(qs, shape), _steps(os_, shape)
+    lp = 0 if lse is None else _flat(lse, torch.float32, device, total * Hq, "lse")
+    lstep = 4 * Hq if lp else 0
+    reqs = []
+    if lists:
+        H = k[0].shape[0] if count else 1
+        for nq, nk, ki, vi in zip(q_lens, kv_lens, k, v):
+            want = (H, nk, d)
+            kp, ks = _strided(ki, dtype, device, want, "k")
+            vp, vs = _strided(vi, dtype, device, want, "v")
+            ks = _steps(ks, want)
+            if ks != _steps(vs, want):
                 raise ValueError("k and v must have the same strides")
-        else:
-            r.k, r.v, r.kv_token_stride, r.kv_head_stride = kp + ko, vp + ko, ks, hs
-            ko += 2 * ks * nk
-        qo += 2 * cfg.q_token_stride * nq
-        oo += 2 * cfg.out_token_stride * nq
-        lo += 4 * Hq * nq
-    wsp = None if ws is None or ws.numel() == 0 else _dev(ws, torch.uint8, 0, "ws")
-    _check(lib().skv_attn_prompt(ctypes.byref(cfg), reqs, count, wsp, 0 if wsp is None else ws.numel(),
-                                 _stream(stream)), "skv_attn_prompt")
+            reqs.append(_ATTN_REQUEST.pack(nq, nk, qp, kp, vp, op, lp, ks[1], ks[0]))
+            qp, op, lp = qp + 2 * qs[0] * nq, op + 2 * os_[0] * nq, lp + lstep * nq
+    else:
+        if k.dim() != 3 or sum(kv_lens) != k.shape[0]:
+            raise ValueError("k must be [tokens][heads][d], kv_lens adding up to its tokens")
+        H = k.shape[1]
+        want = (k.shape[0], H, d)
+        kp, ks = _strided(k, dtype, device, want, "k")
+        vp, vs = _strided(v, dtype, device, want, "v")
+        ks = _steps(ks, want)
+        if ks != _steps(vs, want):
+            raise ValueError("k and v must have the same strides")
+        kstep = 2 * ks[0]
+        for nq, nk in zip(q_lens, kv_lens):
+            reqs.append(_ATTN_REQUEST.pack(nq, nk, qp, kp, vp, op, lp, ks[0], ks[1]))
+            qp, op, lp = qp + 2 * qs[0] * nq, op + 2 * os_[0] * nq, lp + lstep * nq
+            kp, vp = kp + kstep * nk, vp + kstep * nk
+    cfg = _ATTN_CONFIG.pack(_ATTN_TYPES[dtype], Hq, H, d, bool(causal), d ** -0.5 if scale is None else scale,
+                            qs[0], qs[1], os_[0], os_[1])
+    size = 0 if ws is None else ws.numel()
+    wsp = _flat(ws, torch.uint8, device, 0, "ws") if size else None
+    _check(lib().skv_attn_prompt(cfg, b"".join(reqs), count, wsp, size, _stream_on(device, stream)), "skv_attn_prompt")
 
 
 def attn_decode_workspace_size(num_requests: int, num_queries: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
                                max_len: int, prefix_len: int = 0) -> int:
     """Workspace bytes of attn_decode with these arguments."""
-    cfg = DecodeConfig(num_requests=num_requests, num_queries=num_queries, num_q_heads=num_q_heads,
-                       num_kv_heads=num_kv_heads, head_dim=head_dim, max_len=max_len, prefix_len=prefix_len)
+    cfg = _DECODE_CONFIG.pack(DTYPE_F16, num_requests, num_queries, num_q_heads, num_kv_heads, head_dim, 1, 1, 0, max_len,
+                              prefix_len, 0, 1.0, *[0] * 9)
     out = ctypes.c_uint64()
-    _check(lib().skv_attn_decode_workspace_size(ctypes.byref(cfg), ctypes.byref(out)),
-           "skv_attn_decode_workspace_size")
+    _check(lib().skv_attn_decode_workspace_size(cfg, ctypes.byref(out)), "skv_attn_decode_workspace_size")
     return out.value
 
 
@@ -671,63 +681,69 @@ def attn_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, b
     have stride 0); DROP tokens are masked, tokens past tier_len kept.  lse:
     float32 [B][Lq][Hq].  ws: attn_decode_workspace_size bytes.  dev_status:
     int32[1], set on a bad table entry or length, never cleared."""
-    if q.dtype not in _ATTN_TYPES:
-        raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
+    dtype, device = q.dtype, q.get_device()
+    if dtype not in _ATTN_TYPES:
+        raise TypeError(f"q must be float16 or bfloat16, got {dtype}")
     if q.dim() != 4 or k_cache.dim() != 4:
         raise ValueError("q must be [B][Lq][Hq][d] and the caches [num_blocks][block_size][H][d]")
-    B, Lq, Hq, d = q.shape
-    nb, bs, H, _ = k_cache.shape
-    qp, op = _rows(q, q, q.shape, "q"), _rows(out, q, q.shape, "out")
-    kp = _dev(k_cache, q.dtype, nb * bs * H * d, "k_cache")
-    vp = _dev(v_cache, q.dtype, nb * bs * H * d, "v_cache")
-    if k_cache.shape != v_cache.shape or k_cache.shape[3] != d:
+    shape = q.shape
+    B, Lq, Hq, d = shape
+    nb, bs, H, dk = k_cache.shape
+    if dk != d or k_cache.shape != v_cache.shape:
         raise ValueError("caches must be [num_blocks][block_size][H][d] of q's d and alike")
     if block_tables.dim() != 2 or block_tables.shape[0] != B:
         raise ValueError("block_tables must be [B][width]")
-    tp = _dev(block_tables, torch.int32, 0, "block_tables")
-    width = block_tables.shape[1]
+    qp, qs = _strided(q, dtype, device, shape, "q")
+    op, os_ = _strided(out, dtype, device, shape, "out")
+    qs, os_ = _steps(qs, shape), _steps(os_, shape)
+    cells = nb * bs * H * d
+    kp, vp = _flat(k_cache, dtype, device, cells, "k_cache"), _flat(v_cache, dtype, device, cells, "v_cache")
+    tp, width = _flat(block_tables, torch.int32, device, 0, "block_tables"), block_tables.shape[1]
+    tier_p, tier_len, per_request, per_head = None, 0, 0, 0
     if tiers is not None:
-        if not tiers.is_cuda or tiers.dtype != torch.uint8:
-            raise TypeError("tiers must be a uint8 device tensor")
-        n = tiers.shape[-1]
-        if tiers.dim() == 1:
-            tiers = tiers.expand(B, H, n)
-        elif tiers.dim() == 2:
-            tiers = tiers.unsqueeze(1).expand(B, H, n) if tiers.shape[0] == B else tiers
-        if tuple(tiers.shape) != (B, H, n):
+        ts, tier_len = tiers.stride(), tiers.shape[-1] if tiers.dim() else 0
+        if tiers.shape == (tier_len,):
+            pass
+        elif tiers.shape == (B, tier_len):
+            per_request = ts[0]
+        elif tiers.shape == (B, H, tier_len):
+            per_request, per_head = ts[0], ts[1]
+        else:
             raise ValueError("tiers must be [tier_len], [B][tier_len] or [B][H][tier_len]")
-        if n > 1 and tiers.stride(2) != 1:
+        if tiers.dtype != torch.uint8 or tiers.get_device() != device:
+            raise TypeError("tiers must be a uint8 tensor on q's device")
+        if tier_len > 1 and ts[-1] != 1:
             raise ValueError("tiers' last axis must be contiguous")
-    cfg = DecodeConfig(_ATTN_TYPES[q.dtype], B, Lq, Hq, H, d, nb, bs, width, max_len, prefix_len,
-                       0 if tiers is None else tiers.shape[2], d ** -0.5 if scale is None else scale,
-                       _stride(q, 0), _stride(q, 1), _stride(q, 2), _stride(out, 0), _stride(out, 1), _stride(out, 2),
-                       width, 0 if tiers is None else tiers.stride(0), 0 if tiers is None else tiers.stride(1))
-    wsp = None if ws is None or ws.numel() == 0 else _dev(ws, torch.uint8, 0, "ws")
+        tier_p = tiers.data_ptr()
+    cfg = _DECODE_CONFIG.pack(_ATTN_TYPES[dtype], B, Lq, Hq, H, d, nb, bs, width, max_len, prefix_len, tier_len,
+                              d ** -0.5 if scale is None else scale, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], width,
+                              per_request, per_head)
+    size = 0 if ws is None else ws.numel()
     _check(lib().skv_attn_decode(
-        ctypes.byref(cfg), qp, kp, vp, tp, _dev(lens, torch.int32, B, "lens"),
-        None if tiers is None else tiers.data_ptr(), op,
-        None if lse is None else _dev(lse, torch.float32, B * Lq * Hq, "lse"),
-        None if dev_status is None else _dev(dev_status, torch.int32, 1, "dev_status"),
-        wsp, 0 if wsp is None else ws.numel(), _stream(stream)), "skv_attn_decode")
+        cfg, qp, kp, vp, tp, _flat(lens, torch.int32, device, B, "lens"), tier_p, op,
+        None if lse is None else _flat(lse, torch.float32, device, B * Lq * Hq, "lse"),
+        None if dev_status is None else _flat(dev_status, torch.int32, device, 1, "dev_status"),
+        _flat(ws, torch.uint8, device, 0, "ws") if size else None, size, _stream_on(device, stream)), "skv_attn_decode")
 
 
-def _pool(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: Optional[torch.Tensor]) -> PagePool:
+def _pool(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: Optional[torch.Tensor], device: int) -> bytes:
     """The pool of a 16-bit paged cache pair [L][num_blocks][block_size][H][d]."""
-    if k_cache.dim() != 5 or k_cache.shape != v_cache.shape:
+    shape, dtype = k_cache.shape, k_cache.dtype
+    if len(shape) != 5 or shape != v_cache.shape:
         raise ValueError("caches must be [L][num_blocks][block_size][H][d] and alike")
-    if k_cache.dtype not in _ATTN_TYPES:
-        raise TypeError(f"caches must be float16 or bfloat16, got {k_cache.dtype}")
-    L, nb, bs, H, d = k_cache.shape
-    n = k_cache.numel()
-    return PagePool(L, nb, bs, 2 * H * d, _dev(k_cache, k_cache.dtype, n, "k_cache"), _dev(v_cache, k_cache.dtype, n, "v_cache"),
-                    None if refs is None else _dev(refs, torch.int32, nb, "refs"))
+    if dtype not in _ATTN_TYPES:
+        raise TypeError(f"caches must be float16 or bfloat16, got {dtype}")
+    L, nb, bs, H, d = shape
+    return _PAGE_POOL.pack(L, nb, bs, 2 * H * d, _flat(k_cache, dtype, device, 0, "k_cache"),
+                           _flat(v_cache, dtype, device, 0, "v_cache"),
+                           0 if refs is None else _flat(refs, torch.int32, device, nb, "refs"))
 
 
-def _tables(tables: torch.Tensor, rows: int, name: str):
+def _tables(tables: torch.Tensor, rows: int, device: int, name: str):
     """Pointer and width of contiguous block tables int32 [rows][width]."""
     if tables.dim() != 2 or tables.shape[0] != rows:
         raise ValueError(f"{name} must be [{rows}][width]")
-    return _dev(tables, torch.int32, 0, name), tables.shape[1]
+    return _flat(tables, torch.int32, device, 0, name), tables.shape[1]
 
 
 def pages_workspace_size(num_requests: int, num_blocks: int, max_len: int) -> int:
@@ -743,13 +759,14 @@ def pages_reserve(refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, 
                   block_size: int, ws: torch.Tensor, dev_status: torch.Tensor, stream=None):
     """Gives each request the pages to grow from lens to new_lens tokens: the
     lowest free ones (refs 0), written into tables (int32 [B][width])."""
-    B = lens.numel()
-    pool = PagePool(1, refs.numel(), block_size, 16, None, None, _dev(refs, torch.int32, 0, "refs"))
-    tp, width = _tables(tables, B, "tables")
-    _check(lib().skv_pages_reserve(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"),
-                                   _dev(new_lens, torch.int32, B, "new_lens"), B,
-                                   _dev(dev_status, torch.int32, 1, "dev_status"),
-                                   _dev(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)), "skv_pages_reserve")
+    B, device = lens.numel(), refs.get_device()
+    pool = _PAGE_POOL.pack(1, refs.numel(), block_size, 16, 0, 0, _flat(refs, torch.int32, device, 0, "refs"))
+    tp, width = _tables(tables, B, device, "tables")
+    _check(lib().skv_pages_reserve(pool, tp, width, _flat(lens, torch.int32, device, B, "lens"),
+                                   _flat(new_lens, torch.int32, device, B, "new_lens"), B,
+                                   _flat(dev_status, torch.int32, device, 1, "dev_status"),
+                                   _flat(ws, torch.uint8, device, 0, "ws"), ws.numel(), _stream_on(device, stream)),
+           "skv_pages_reserve")
 
 
 def pages_fork(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor,
@@ -757,15 +774,16 @@ def pages_fork(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tensor,
                ws: torch.Tensor, dev_status: torch.Tensor, stream=None):
     """Child c becomes a copy of request parents[c]: full pages shared, a partly
     filled last page copied.  Writes out_tables [children][width] and out_lens."""
-    B, N = lens.numel(), parents.numel()
-    pool = _pool(k_cache, v_cache, refs)
-    tp, width = _tables(tables, B, "tables")
-    op, out_width = _tables(out_tables, N, "out_tables")
-    _check(lib().skv_pages_fork(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"), B,
-                                _dev(parents, torch.int32, N, "parents"), N, op, out_width,
-                                _dev(out_lens, torch.int32, N, "out_lens"),
-                                _dev(dev_status, torch.int32, 1, "dev_status"),
-                                _dev(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)), "skv_pages_fork")
+    B, N, device = lens.numel(), parents.numel(), refs.get_device()
+    pool = _pool(k_cache, v_cache, refs, device)
+    tp, width = _tables(tables, B, device, "tables")
+    op, out_width = _tables(out_tables, N, device, "out_tables")
+    _check(lib().skv_pages_fork(pool, tp, width, _flat(lens, torch.int32, device, B, "lens"), B,
+                                _flat(parents, torch.int32, device, N, "parents"), N, op, out_width,
+                                _flat(out_lens, torch.int32, device, N, "out_lens"),
+                                _flat(dev_status, torch.int32, device, 1, "dev_status"),
+                                _flat(ws, torch.uint8, device, 0, "ws"), ws.numel(), _stream_on(device, stream)),
+           "skv_pages_fork")
 
 
 def pages_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tensor, tables: torch.Tensor,
@@ -775,42 +793,46 @@ def pages_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tens
     [B][tier_len], any request stride; tokens past tier_len are kept): full
     pages before the first dropped token shared, the other rows gathered into
     new pages."""
-    B = lens.numel()
-    pool = _pool(k_cache, v_cache, refs)
-    tp, width = _tables(tables, B, "tables")
-    op, out_width = _tables(out_tables, B, "out_tables")
-    if not tiers.is_cuda or tiers.dtype != torch.uint8:
-        raise TypeError("tiers must be a uint8 device tensor")
+    B, device = lens.numel(), refs.get_device()
+    pool = _pool(k_cache, v_cache, refs, device)
+    tp, width = _tables(tables, B, device, "tables")
+    op, out_width = _tables(out_tables, B, device, "out_tables")
+    if tiers.get_device() != device or tiers.dtype != torch.uint8:
+        raise TypeError("tiers must be a uint8 tensor on the pool's device")
     if tiers.dim() != 2 or tiers.shape[0] != B or (tiers.shape[1] > 1 and tiers.stride(1) != 1):
         raise ValueError("tiers must be [requests][tier_len], its last axis contiguous")
-    _check(lib().skv_pages_compact(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"), B,
+    _check(lib().skv_pages_compact(pool, tp, width, _flat(lens, torch.int32, device, B, "lens"), B,
                                    tiers.data_ptr(), tiers.shape[1], tiers.stride(0), op, out_width,
-                                   _dev(out_lens, torch.int32, B, "out_lens"),
-                                   _dev(dev_status, torch.int32, 1, "dev_status"),
-                                   _dev(ws, torch.uint8, 0, "ws"), ws.numel(), _stream(stream)), "skv_pages_compact")
+                                   _flat(out_lens, torch.int32, device, B, "out_lens"),
+                                   _flat(dev_status, torch.int32, device, 1, "dev_status"),
+                                   _flat(ws, torch.uint8, device, 0, "ws"), ws.numel(), _stream_on(device, stream)),
+           "skv_pages_compact")
 
 
 def pages_free(refs: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, block_size: int,
                dev_status: torch.Tensor, stream=None):
     """Releases requests: the count of every page they hold goes down by one."""
-    B = lens.numel()
-    pool = PagePool(1, refs.numel(), block_size, 16, None, None, _dev(refs, torch.int32, 0, "refs"))
-    tp, width = _tables(tables, B, "tables")
-    _check(lib().skv_pages_free(ctypes.byref(pool), tp, width, _dev(lens, torch.int32, B, "lens"), B,
-                                _dev(dev_status, torch.int32, 1, "dev_status"), _stream(stream)), "skv_pages_free")
+    B, device = lens.numel(), refs.get_device()
+    pool = _PAGE_POOL.pack(1, refs.numel(), block_size, 16, 0, 0, _flat(refs, torch.int32, device, 0, "refs"))
+    tp, width = _tables(tables, B, device, "tables")
+    _check(lib().skv_pages_free(pool, tp, width, _flat(lens, torch.int32, device, B, "lens"), B,
+                                _flat(dev_status, torch.int32, device, 1, "dev_status"), _stream_on(device, stream)),
+           "skv_pages_free")
 
 
 def pages_copy(src_k: torch.Tensor, src_v: torch.Tensor, dst_k: torch.Tensor, dst_v: torch.Tensor,
                src_pages: torch.Tensor, dst_pages: torch.Tensor, dev_status: torch.Tensor, stream=None):
     """Copies page src_pages[i] of one cache pair to page dst_pages[i] of another
     in every layer."""
-    src, dst = _pool(src_k, src_v, None), _pool(dst_k, dst_v, None)
+    device = src_k.get_device()
+    src, dst = _pool(src_k, src_v, None, device), _pool(dst_k, dst_v, None, device)
     if src_k.shape[2:] != dst_k.shape[2:] or src_k.shape[0] != dst_k.shape[0] or src_k.dtype != dst_k.dtype:
         raise ValueError("the caches must agree in layers, block size, heads, dimension and type")
     n = src_pages.numel()
-    _check(lib().skv_pages_copy(ctypes.byref(src), ctypes.byref(dst), _dev(src_pages, torch.int32, n, "src_pages"),
-                                _dev(dst_pages, torch.int32, n, "dst_pages"), n,
-                                _dev(dev_status, torch.int32, 1, "dev_status"), _stream(stream)), "skv_pages_copy")
+    _check(lib().skv_pages_copy(src, dst, _flat(src_pages, torch.int32, device, n, "src_pages"),
+                                _flat(dst_pages, torch.int32, device, n, "dst_pages"), n,
+                                _flat(dev_status, torch.int32, device, 1, "dev_status"), _stream_on(device, stream)),
+           "skv_pages_copy")
 
 
 def link(dst: torch.Tensor, src: torch.Tensor, nbytes: int, host_staging: Optional[torch.Tensor] = None,
