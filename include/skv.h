@@ -611,7 +611,8 @@ typedef struct skv_decode_config {
   int32_t dtype;         /* SKV_DTYPE_* of q, the cache and out                   */
   int32_t num_requests;  /* B                                                     */
   int32_t num_queries;   /* Lq: newest tokens of each request, already in the
-                            cache (1; more to verify drafted tokens)              */
+                            cache (1; more to verify drafted tokens; 0: nothing
+                            to do)                                                */
   int32_t num_q_heads, num_kv_heads, head_dim; /* as skv_attn_config              */
   int32_t num_blocks, block_size;              /* num_blocks * block_size < 2^31  */
   int32_t table_width;   /* entries of a request's block table                    */

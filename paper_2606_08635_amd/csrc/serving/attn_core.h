@@ -219,9 +219,9 @@ struct WaveAttention {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) q[s] = __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4*>(p + 32 * s));
   }
-  // Waits for Q; to be called before the first direct load.  The compiler's own wait
-  // would sit in the tile loop, where it would also wait for the direct loads that it
-  // does not know of.
+  // Waits for Q (and every other load) before the tile loop.  The compiler's own wait
+  // would sit in the loop, where it would also wait for the direct loads that it does
+  // not know of.
   __device__ __forceinline__ void wait_q() {
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
 #pragma unroll
@@ -552,24 +552,29 @@ struct WaveAttention {
     return on && ks < (F == kPair ? 2 : 1);
   }
   __device__ __forceinline__ void write_state(uint8_t* to) const {
-    float* f = reinterpret_cast<float*>(to) + (threadIdx.x & 63);
-    f[0] = m;
-    f[64] = l;
+    floatx4* f = reinterpret_cast<floatx4*>(to) + (threadIdx.x & 63);
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) f[64 * (2 + 16 * dt + r)] = o[dt][r];
+      for (int r = 0; r < 4; ++r)
+        f[64 * (4 * dt + r)] = floatx4{o[dt][4 * r], o[dt][4 * r + 1], o[dt][4 * r + 2], o[dt][4 * r + 3]};
+    reinterpret_cast<floatx2*>(f - (threadIdx.x & 63) + 64 * 4 * kTiles)[threadIdx.x & 63] = floatx2{m, l};
   }
   __device__ __forceinline__ void merge_state(const uint8_t* from) {
-    const float* f = reinterpret_cast<const float*>(from) + (threadIdx.x & 63);
-    const float m2 = f[0], mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.0f : mn;
-    const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(m2 - ref);
+    const floatx4* f = reinterpret_cast<const floatx4*>(from) + (threadIdx.x & 63);
+    const floatx2 ml = reinterpret_cast<const floatx2*>(f - (threadIdx.x & 63) + 64 * 4 * kTiles)[threadIdx.x & 63];
+    const float mn = fmaxf(m, ml.x), ref = mn == -INFINITY ? 0.0f : mn;
+    const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(ml.x - ref);
     m = mn;
-    l = l * a + f[64] * b;
+    l = l * a + ml.y * b;
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[dt][r] = o[dt][r] * a + f[64 * (2 + 16 * dt + r)] * b;
+      for (int r = 0; r < 4; ++r) {
+        const floatx4 x = f[64 * (4 * dt + r)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[dt][4 * r + i] = o[dt][4 * r + i] * a + x[i] * b;
+      }
   }
   // Whether this lane writes the row's reference and sum, or its lse.
   __device__ __forceinline__ bool writes_sum() const { return (threadIdx.x & 32) == 0 && ks == 0; }
@@ -612,6 +617,7 @@ __device__ __forceinline__ void walk_once(Wave& w, int t0, int t1, Issue issue, 
   constexpr int kBytes = Stage<D>::kBytes;
   const std::integral_constant<bool, SECOND> second;
   if (t0 < t1) issue(t0, 0);
+  w.wait_q();
   if constexpr (2 * kBytes <= 65536) {  // both buffers within an instruction's offset
     for (int t = t0; t < t1; t += 2) {
       wait_direct_loads();

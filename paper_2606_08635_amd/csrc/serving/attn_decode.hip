@@ -5,9 +5,8 @@
 //   prefix  all B Lq G rows of a KV head (128 per workgroup) against the shared
 //           positions, so a key is loaded once per row block and not per request;
 //   rest    the Lq G rows of one request against its own positions.
-// The prefix is cut into equal parts and the requests' rests, one behind the other,
-// into equal slices, so that the work is even whatever the lengths; a second launch
-// joins a row's parts.  A workgroup turns its range into a list of cache rows in shared memory
+// The prefix is cut into equal parts, the requests' rests into parts of one length
+// that the device finds from their lengths; a second launch joins a row's parts.  A workgroup turns its range into a list of cache rows in shared memory
 // first (up to kList positions at a time): positions past the request's end and
 // DROP tokens are left out, so the tiles that follow hold kept tokens only and a
 // dropped token costs neither bandwidth nor a product.  The tiles gather the
@@ -151,7 +150,6 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
         w.template tile<decltype(offset)::value, decltype(again)::value>(area, a.alpha, t * S::kKeys, active, tiles < 4,
                                                                           masked, shown);
       };
-      w.wait_q();
       if (q1 < p1) next.load(a, table, tiers, q1, min(p1, q1 + kList));
       walk_once<D, decltype(second)::value>(w, 0, nt, issue, tile);
       if (q1 < p1) __syncthreads();  // the next list
@@ -200,109 +198,112 @@ __device__ __forceinline__ Place place(uint32_t i, uint32_t runs, uint32_t block
   return p;
 }
 
+// Where a tail workgroup's part lies: request and tiles of its tail.
+struct TailPart {
+  int request, first, last;
+};
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_inclusive_scan(x)), 63));
+}
+// Cuts the tails into parts of c tiles, c the smallest (from 2 on) that gives at most
+// a.tail_parts parts, and finds part `at`; false past the last.  Every wave does it
+// for itself, a lane holding four requests, so nothing waits for another wave.
+// `tell`: write the requests' first parts and counts for the join.
+__device__ __forceinline__ bool find_part(const DecodeArgs& a, int at, bool tell, TailPart& part) {
+  const int lane = threadIdx.x & 63;
+  uint32_t n[4], all = 0, most = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n[i] = 4 * lane + i < a.B ? static_cast<uint32_t>(tail_tokens(a, 4 * lane + i) + 63) / 64 : 0;
+    all += n[i];
+    most = max(most, n[i]);
+  }
+  all = wave_sum(all);
+  most = wave_max(most);
+  const uint32_t limit = static_cast<uint32_t>(a.tail_parts);
+  uint32_t lo = max(2u, (all + limit - 1) / limit), hi = max(lo, most);  // hi gives one part per request
+  while (lo < hi) {
+    const uint32_t c = (lo + hi) >> 1;
+    uint32_t parts = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) parts += (n[i] + c - 1) / c;
+    if (wave_sum(parts) <= limit) hi = c;
+    else lo = c + 1;
+  }
+  uint32_t mine = 0, count[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    count[i] = (n[i] + lo - 1) / lo;
+    mine += count[i];
+  }
+  uint32_t begin = wave_inclusive_scan(mine) - mine;
+  int request = -1;
+  uint32_t first = 0, tiles = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = static_cast<uint32_t>(at) - begin;  // (wraps where the part lies before)
+    if (u < count[i]) {
+      request = 4 * lane + i;
+      first = u * lo;
+      tiles = n[i];
+    }
+    if (tell && 4 * lane + i < a.B) {
+      a.first_part[4 * lane + i] = static_cast<int32_t>(begin);
+      a.part_count[4 * lane + i] = static_cast<int32_t>(count[i]);
+    }
+    begin += count[i];
+  }
+  const uint64_t has = __ballot(request >= 0);
+  if (has == 0) return false;
+  const int from = __builtin_ctzll(has);
+  part.request = __builtin_amdgcn_readlane(request, from);
+  part.first = __builtin_amdgcn_readlane(static_cast<int>(first), from);
+  part.last = min(part.first + static_cast<int>(lo), __builtin_amdgcn_readlane(static_cast<int>(tiles), from));
+  return true;
+}
+
 template <class E, int D>
 __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void attn_decode(const DecodeArgs a) {
   constexpr Form F = D >= 256 ? kPair : kOne;
   __shared__ __align__(1024) uint8_t stage[2 * Stage<D>::kBytes];
   __shared__ typename WaveAttention<E, D, F>::AreaType area;
   __shared__ Lists<Stage<D>::kThreads> lists;
-  __shared__ int32_t ends[kSlicedRequests];  // tiles of the tails up to each request's end
-  uint32_t at = blockIdx.x;
   const uint32_t H = static_cast<uint32_t>(a.H);
   const int own = a.Lq * a.G, rows_all = a.B * own;
-  int h, blk, tiles, b = 0, t = 0, t1 = 1;  // tail: request and tiles of the slice
-  const bool prefix = at < a.prefix_groups;
-  if (prefix) {
-    const uint32_t parts = static_cast<uint32_t>(a.prefix_parts);
-    const Place p = place<D>(at, parts, static_cast<uint32_t>(a.prefix_blocks), H);
-    t = static_cast<int>(p.run);
-    t1 = t + 1;
-    blk = static_cast<int>(p.blk);
+  int h, row0, rows, tiles, p0, p1, b = 0;
+  int64_t part_row;
+  if (blockIdx.x < a.prefix_groups) {
+    const Place p = place<D>(blockIdx.x, static_cast<uint32_t>(a.prefix_parts), static_cast<uint32_t>(a.prefix_blocks), H);
     h = static_cast<int>(p.h);
     tiles = a.prefix_tiles;
+    row0 = static_cast<int>(p.blk) * tiles * 32;
+    rows = min(tiles * 32, rows_all - row0);
+    p0 = static_cast<int>(p.run) * a.prefix_chunk;
+    p1 = min(a.prefix, p0 + a.prefix_chunk);
+    part_row = (static_cast<int64_t>(p.run) * a.H + h) * rows_all + row0;
   } else {
-    const uint32_t runs = static_cast<uint32_t>(a.slices == 0 ? a.B : a.slices);
-    const Place p = place<D>(at - a.prefix_groups, runs, static_cast<uint32_t>(a.tail_blocks), H);
-    at = p.run;
-    blk = static_cast<int>(p.blk);
+    const uint32_t runs = static_cast<uint32_t>(a.tail_parts == 0 ? a.B : a.tail_parts);
+    const Place p = place<D>(blockIdx.x - a.prefix_groups, runs, static_cast<uint32_t>(a.tail_blocks), H);
     h = static_cast<int>(p.h);
     tiles = a.tail_tiles;
-    if (a.slices == 0) {
-      b = static_cast<int>(at);
+    p0 = a.prefix;
+    if (a.tail_parts == 0) {
+      b = static_cast<int>(p.run);
+      p1 = a.prefix + tail_tokens(a, b);
     } else {
-      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, me = threadIdx.x;
-      const int n = me < a.B ? (tail_tokens(a, me) + 63) / 64 : 0;
-      const uint32_t inc = wave_inclusive_scan(static_cast<uint32_t>(n));
-      if (lane == 63) lists.scan[wave] = inc;
-      __syncthreads();
-      int end = static_cast<int>(inc), all = 0;
-#pragma unroll
-      for (int w = 0; w < kSlicedRequests / 64; ++w) {
-        if (w < wave) end += static_cast<int>(lists.scan[w]);
-        all += static_cast<int>(lists.scan[w]);
-      }
-      if (me < kSlicedRequests) ends[me] = end;
-      const int runs = min(a.slices, max(all, 1));  // a tile at least to each: every slice of a request has a part
-      auto start_of = [&](int s) { return static_cast<int>(static_cast<int64_t>(all) * s / runs); };
-      if (blockIdx.x == a.prefix_groups && me < a.B) {  // for the join
-        // the slice of tile x is the last one that starts at or before it
-        auto slice_of = [&](int x) {
-          int s = static_cast<int>(static_cast<int64_t>(x) * runs / all);
-          while (s + 1 < runs && start_of(s + 1) <= x) ++s;
-          return s;
-        };
-        const int s0 = n > 0 ? slice_of(end - n) : -1;
-        a.first_slice[me] = s0;
-        a.part_count[me] = n > 0 ? slice_of(end - 1) - s0 + 1 : 0;
-      }
-      __syncthreads();
-      if (static_cast<int>(at) >= runs) return;
-      t = start_of(static_cast<int>(at));
-      t1 = start_of(static_cast<int>(at) + 1);
-      int hi = a.B - 1;  // the first request that ends behind tile t
-      while (b < hi) {
-        const int mid = (b + hi) >> 1;
-        if (ends[mid] > t) hi = mid;
-        else b = mid + 1;
-      }
+      TailPart part;
+      if (!find_part(a, static_cast<int>(p.run), blockIdx.x == a.prefix_groups && threadIdx.x < 64, part)) return;
+      b = part.request;
+      p1 = a.prefix + min(tail_tokens(a, b), 64 * part.last);
+      p0 += 64 * part.first;
     }
+    row0 = b * own + static_cast<int>(p.blk) * tiles * 32;
+    rows = min(tiles * 32, own - static_cast<int>(p.blk) * tiles * 32);
+    part_row = a.direct ? -1 : a.tail_at + (static_cast<int64_t>(p.run) * a.H + h) * own + static_cast<int>(p.blk) * tiles * 32;
   }
-  const int slice = static_cast<int>(at);
-  while (t < t1) {
-    int row0, rows, p0, p1;
-    int64_t part_row;
-    const int32_t* table = a.tables + b * a.table_stride;
-    const uint8_t* tiers = a.tiers == nullptr ? nullptr : a.tiers + b * a.tier_request + h * a.tier_head;
-    if (prefix) {
-      row0 = blk * tiles * 32;
-      rows = min(tiles * 32, rows_all - row0);
-      p0 = t * a.prefix_chunk;
-      p1 = min(a.prefix, p0 + a.prefix_chunk);
-      part_row = (static_cast<int64_t>(t) * a.H + h) * rows_all + row0;
-      ++t;
-    } else {
-      row0 = b * own + blk * tiles * 32;
-      rows = min(tiles * 32, own - blk * tiles * 32);
-      const int n = tail_tokens(a, b);
-      if (a.slices == 0) {
-        p0 = a.prefix;
-        p1 = a.prefix + n;
-        t = t1;
-      } else {
-        const int begin = b > 0 ? ends[b - 1] : 0, stop = min(t1, ends[b]);
-        p0 = a.prefix + 64 * (t - begin);
-        p1 = a.prefix + min(n, 64 * (stop - begin));
-        t = stop;
-      }
-      part_row = a.direct ? -1
-                          : a.tail_at + (static_cast<int64_t>(a.slices == 0 ? b : slice + b) * a.H + h) * own + blk * tiles * 32;
-    }
-    attend<E, D, F>(a, stage, area, lists, h, row0, rows, tiles, table, tiers, p0, p1, part_row);
-    if (t >= t1) break;
-    __syncthreads();  // the stage and the lists are free
-    do ++b;  // the next request with a tail
-    while (b < a.B - 1 && ends[b] <= t);
-  }
+  const int32_t* table = a.tables + b * a.table_stride;
+  const uint8_t* tiers = a.tiers == nullptr ? nullptr : a.tiers + b * a.tier_request + h * a.tier_head;
+  attend<E, D, F>(a, stage, area, lists, h, row0, rows, tiles, table, tiers, p0, p1, part_row);
 }
 
 // Joins the parts of each row: WAVES waves per (KV head, row).
@@ -319,10 +320,10 @@ __global__ __launch_bounds__(256) void attn_decode_join(const DecodeArgs a) {
   const uint32_t b = a.by_Lq.div(token), i = token - b * a.Lq;
   JoinedRow<D, WAVES> j;
   j.add(a.part_o, a.part_ml, at, rows * a.H, a.prefix_parts);
-  const int slice = a.slices == 0 ? 0 : a.first_slice[b];
   const int64_t stride = static_cast<int64_t>(a.H) * own;
-  j.add(a.part_o, a.part_ml, a.tail_at + (static_cast<int64_t>(slice) + b) * stride + static_cast<int64_t>(h) * own + (row - b * own),
-        stride, a.slices == 0 ? 1 : a.part_count[b]);
+  const int64_t first = a.tail_parts == 0 ? b : a.first_part[b];
+  j.add(a.part_o, a.part_ml, a.tail_at + first * stride + static_cast<int64_t>(h) * own + (row - b * own), stride,
+        a.tail_parts == 0 ? 1 : a.part_count[b]);
   if (!j.together(shared)) return;
   const int head = h * a.G + static_cast<int>(g);
   j.template write<E>(reinterpret_cast<typename E::elem*>(a.out + b * a.out_request + i * a.out_token + head * a.out_head));

@@ -79,7 +79,6 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
         area, a.alpha, key0, active && key0 <= wave_max, false, [&](int key, int keys) { return key + keys - 1 > wave_min; },
         [&](int key) { return key <= limit; });
   };
-  w.wait_q();
   walk_tiles(w, area, [&](auto second) { walk_once<D, decltype(second)::value>(w, t0, t1, issue, tile); });
   const bool writes = w.finish(stage, area, active);
   if (!writes || row0 + (lane & 31) >= rows) return;  // (both lane-halves of a row stay: write_out pairs them)

@@ -428,7 +428,7 @@ __global__ __launch_bounds__(256) void pages_copy(const PageCopyArgs a, uint32_t
 
 hipError_t launch_pages(const PageArgs& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
-  if (a.op == kPagesCompact) {
+  if (a.op == kPagesCompact && a.rows > 0) {
     pages_check<<<static_cast<uint32_t>(a.rows) * static_cast<uint32_t>((a.chunks + 3) / 4), 256, 0, stream>>>(a);
     e = hipGetLastError();
   } else if (a.op == kPagesFork && a.checked) {
@@ -439,6 +439,7 @@ hipError_t launch_pages(const PageArgs& a, hipStream_t stream) {
   pages_plan<<<1, kPlanThreads, 0, stream>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || a.op == kPagesReserve) return e;
   const uint64_t entries = (static_cast<uint64_t>(a.rows) * a.out_width + 1023) / 1024;
+  if (a.rows == 0) return hipSuccess;
   pages_apply<<<static_cast<uint32_t>(a.copy_groups + entries), 256, 0, stream>>>(a);
   return hipGetLastError();
 }

@@ -126,12 +126,13 @@ skv_status prompt_launches(const skv_attn_config* c, const skv_attn_request* req
 // How skv_attn_decode cuts its work (the counts, lengths and dimensions of c are
 // valid).
 struct DecodePlan {
-  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, slices, tail_blocks, tail_tiles;
+  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, tail_parts, tail_blocks, tail_tiles;
   uint64_t prefix_groups, groups, prefix_rows, part_rows, bytes;  // (bytes 0: no parts)
 };
 
 DecodePlan plan_decode(const skv_decode_config* c) {
   DecodePlan p{};
+  if (c->num_requests == 0 || c->num_queries == 0) return p;
   const int64_t H = c->num_kv_heads, G = c->num_q_heads / H, own = c->num_queries * G, all = own * c->num_requests;
   const int64_t tail = std::max(0, c->max_len - c->prefix_len);
   const int64_t room = c->head_dim >= 256 ? kCus : 2 * kCus;  // workgroups that the GPU holds at once
@@ -152,20 +153,19 @@ DecodePlan plan_decode(const skv_decode_config* c) {
     p.prefix_groups = static_cast<uint64_t>(H * p.prefix_blocks * p.prefix_parts);
     p.prefix_rows = static_cast<uint64_t>(p.prefix_parts * H * all);
   }
-  // The tails in slices that fill the rest of the room, of 128 tokens at least (as far
-  // as max_len says), unless the requests fill it as they are and are short: a
-  // slice's further requests cost it about 5 us each (64 requests of up to 400 tokens:
-  // 14 us whole, 36 in slices), uneven lengths cost more from 2048 tokens on.
-  const int64_t groups = H * p.tail_blocks;
-  const int64_t left = std::max<int64_t>(1, room - static_cast<int64_t>(p.prefix_groups));
-  const int64_t slices = std::min(std::max<int64_t>(1, left / groups), up(c->num_requests * tail, 128));
-  const bool whole = tail <= 256 || (tail < 2048 && c->num_requests * groups * 4 >= left * 3);
-  if (c->num_requests <= kSlicedRequests && !whole && slices > 1) p.slices = static_cast<int32_t>(slices);
-  const int64_t runs = p.slices > 0 ? p.slices : c->num_requests;
+  // The tails in as many parts as fill the rest of the room, two per request at least
+  // where they may be long and uneven, and not more than 128 tokens each would give
+  // (as far as max_len says); whole where that fills the room with short ones (64
+  // requests of up to 400 tokens: 14 us whole, 20 with a second launch for the parts).
+  const int64_t groups = H * p.tail_blocks, left = room - static_cast<int64_t>(p.prefix_groups);
+  int64_t parts = std::max(left / groups, c->num_requests * static_cast<int64_t>(tail >= 2048 ? 2 : 1));
+  parts = std::min(parts, c->num_requests * up(tail, 128));
+  const bool whole = tail <= 256 || (tail < 2048 && c->num_requests * groups >= left);
+  if (c->num_requests <= kCutRequests && !whole && parts > 1) p.tail_parts = static_cast<int32_t>(parts);
+  const int64_t runs = p.tail_parts > 0 ? p.tail_parts : c->num_requests;
   p.groups = p.prefix_groups + static_cast<uint64_t>(groups * runs);
-  if (p.prefix_parts == 0 && p.slices == 0) return p;
-  const int64_t places = p.slices > 0 ? p.slices + c->num_requests : c->num_requests;
-  p.part_rows = p.prefix_rows + static_cast<uint64_t>(places * H * own);
+  if (p.prefix_parts == 0 && p.tail_parts == 0) return p;
+  p.part_rows = p.prefix_rows + static_cast<uint64_t>(runs * H * own);
   p.bytes = p.part_rows * static_cast<uint64_t>(c->head_dim + 2) * 4u + 8u * static_cast<uint64_t>(c->num_requests);
   return p;
 }
@@ -173,7 +173,7 @@ DecodePlan plan_decode(const skv_decode_config* c) {
 skv_status check_decode_sizes(const skv_decode_config* c) {
   if (c == nullptr || !shape_ok(SKV_DTYPE_F16, c->num_q_heads, c->num_kv_heads, c->head_dim, 1.0f))
     return SKV_ERR_INVALID_ARG;
-  if (c->num_requests < 0 || c->num_queries < 1 || c->max_len < 0 || c->prefix_len < 0) return SKV_ERR_INVALID_ARG;
+  if (c->num_requests < 0 || c->num_queries < 0 || c->max_len < 0 || c->prefix_len < 0) return SKV_ERR_INVALID_ARG;
   if (static_cast<int64_t>(c->num_requests) * c->num_queries > (1 << 20) ||
       static_cast<int64_t>(c->num_requests) * c->num_queries * c->num_q_heads > (1 << 26))
     return SKV_ERR_INVALID_ARG;
@@ -356,7 +356,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
       !stride_ok(c.out_request_stride) || !stride_ok(c.out_token_stride) || !stride_ok(c.out_head_stride))
     return SKV_ERR_INVALID_ARG;
   if (tiers != nullptr && (c.tier_len < 0 || c.tier_request_stride < 0 || c.tier_head_stride < 0)) return SKV_ERR_INVALID_ARG;
-  if (c.num_requests == 0) return SKV_OK;
+  if (c.num_requests == 0 || c.num_queries == 0) return SKV_OK;
   if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(lens, 4) ||
       !aligned(tables, 4) || (lse != nullptr && !aligned(lse, 4)) || (dev_status != nullptr && !aligned(dev_status, 4)))
     return SKV_ERR_INVALID_ARG;
@@ -379,8 +379,8 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   a.direct = p.bytes == 0;
   if (!a.direct) {
     a.part_ml = a.part_o + p.part_rows * static_cast<uint64_t>(c.head_dim);
-    a.first_slice = reinterpret_cast<int32_t*>(a.part_ml + 2 * p.part_rows);
-    a.part_count = a.first_slice + c.num_requests;
+    a.first_part = reinterpret_cast<int32_t*>(a.part_ml + 2 * p.part_rows);
+    a.part_count = a.first_part + c.num_requests;
   }
   a.tail_at = static_cast<int64_t>(p.prefix_rows);
   a.q_request = c.q_request_stride;
@@ -405,7 +405,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   a.prefix_blocks = p.prefix_blocks;
   a.prefix_tiles = p.prefix_tiles;
   a.prefix_chunk = p.prefix_chunk;
-  a.slices = p.slices;
+  a.tail_parts = p.tail_parts;
   a.tail_blocks = p.tail_blocks;
   a.tail_tiles = p.tail_tiles;
   a.prefix_groups = static_cast<uint32_t>(p.prefix_groups);

@@ -42,12 +42,11 @@ hipError_t launch_attn_prompt(const PromptArgs& a, int32_t dtype, int32_t d, hip
 
 // Attention of a batch's newest tokens over the paged cache.  The launch's
 // workgroups are first those of the shared prefix (row blocks x KV heads x
-// parts, over the rows of every request), then those of the rest ("tails") of the
-// requests (slices x row blocks x KV heads): with slices == 0 a slice is a request;
-// else the tails, in whole tiles and one behind the other, are cut into `slices`
-// equal runs, so that the work is even whatever the lengths (at most
-// kSlicedRequests requests).
-constexpr int kSlicedRequests = 256;
+// parts, over the rows of every request), then those of the rest ("tail") of each
+// request (parts x row blocks x KV heads): with tail_parts == 0 a part is a request;
+// else the device cuts the tails of at most kCutRequests requests into at most
+// tail_parts parts, as short as that allows.
+constexpr int kCutRequests = 256;
 struct DecodeArgs {
   const uint16_t* q;
   const uint16_t* k;
@@ -59,17 +58,16 @@ struct DecodeArgs {
   const uint8_t* tiers;   // may be null
   uint32_t* status;       // may be null
   // partial results, unnormalized sums and (reference, sum): prefix rows [parts][H]
-  // [B Lq G], then tail rows [slice + request][H][Lq G] (a slice's run over the
-  // requests makes every slice + request a place of its own)
+  // [B Lq G], then tail rows [part][H][Lq G]
   float* part_o;
   float* part_ml;
-  int32_t* first_slice;  // [B]: slice of a request's first part; -1: no tail
-  int32_t* part_count;   // [B]
+  int32_t* first_part;  // [B]: a request's first tail part, and how many it has
+  int32_t* part_count;
   int64_t q_request, q_token, q_head, out_request, out_token, out_head, table_stride, tier_request, tier_head;
   int64_t tail_at;       // first tail row of the partial results
   int32_t B, Lq, H, G, num_blocks, block_size, width, prefix, tier_len;
   int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk;  // row blocks, 32-row tiles of one, tokens of a part
-  int32_t slices, tail_blocks, tail_tiles;
+  int32_t tail_parts, tail_blocks, tail_tiles;
   int32_t direct;                  // no parts: results are written at once
   uint32_t prefix_groups, groups;  // workgroups of the prefix, of the launch
   float alpha;

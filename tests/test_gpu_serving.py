@@ -1,0 +1,224 @@
+"""The attention and page operators with the codec, as a server would run them:
+a prompt's attention, its K and V packed and unpacked into reserved pages, decode
+over the paged cache with its dropped tokens masked, the same after compaction,
+forks that share the prompt, and everything released."""
+import pytest
+import torch
+
+from attn_reference import attention, causal, check
+from paper_2606_08635_amd import skv, workloads
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.mark.parametrize("model,budget", [((2, 4, 2, 64), 0.3), ((3, 8, 2, 128), 0.2), ((1, 4, 4, 256), 0.3)])
+def test_prompt_to_forked_decode(model, budget):
+    L, Hq, H, d = model
+    block, n, children, steps = 16, 523, 3, 5
+    k, v = workloads.make_kv(L, H, n, d, seed=1, device=DEV)
+    # prefill: attention over the prompt straight from the codec's buffers
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn(n, Hq, d, generator=g).half()
+    out, lse = torch.empty(n, Hq, d, dtype=torch.float16, device=DEV), torch.empty(n, Hq, device=DEV)
+    skv.attn_prompt(q.to(DEV), [k[0]], [v[0]], out, [n], lse=lse)
+    kc0, vc0 = k[0].transpose(0, 1).cpu(), v[0].transpose(0, 1).cpu()
+    check(out, lse, attention(q, kc0, vc0, causal(n, n), d ** -0.5), "prefill")
+    # handoff at a budget that drops tokens, into pages that the pool gives
+    cfg = skv.config(L, H, d, n, budget, num_tiers=2)
+    codec = skv.Codec(cfg, DEV)
+    payload = codec.encode(k, v)
+    nb, width = 200, -(-(n + steps) // block)
+    kc, vc = (torch.full((L, nb, block, H, d), float("nan"), dtype=torch.float16, device=DEV) for _ in range(2))
+    refs = torch.zeros(nb, dtype=torch.int32, device=DEV)
+    refs[::3] = 1  # pages of others
+    others = refs.clone()
+    ws = torch.empty(skv.pages_workspace_size(8, nb, width * block), dtype=torch.uint8, device=DEV)
+    status = torch.full((8,), -1, dtype=torch.int32, device=DEV)
+    tables = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    lens = torch.tensor([n], dtype=torch.int32, device=DEV)
+    skv.pages_reserve(refs, tables, torch.zeros_like(lens), lens, block, ws, status[0:1])
+    codec.decode(payload, kc, vc, tables[0], block)
+    assert (codec.tier == skv.DROP).any()
+    # compaction: the same request without its dropped tokens
+    small = torch.full_like(tables, -1)
+    small_lens = torch.zeros_like(lens)
+    skv.pages_compact(kc, vc, refs, tables, lens, codec.tier[None], small, small_lens, ws, status[1:2])
+    kept = int((codec.tier != skv.DROP).sum())
+    assert small_lens.item() == kept
+    # children of both, with room for tokens of their own, which are written
+    parents = torch.zeros(children, dtype=torch.int32, device=DEV)
+    rows = {}
+    for name, t, ln in (("full", tables, lens), ("small", small, small_lens)):
+        kt, kl = torch.full((children, width), -1, dtype=torch.int32, device=DEV), torch.zeros_like(parents)
+        i = 2 if name == "full" else 5
+        skv.pages_fork(kc, vc, refs, t, ln, parents, kt, kl, ws, status[i:i + 1])
+        new = kl + steps
+        skv.pages_reserve(refs, kt, kl, new, block, ws, status[i + 1:i + 2])
+        at = kl.long()[:, None] + torch.arange(steps, device=DEV)
+        page = kt.long().gather(1, at // block)
+        own = torch.randn(2, L, children, steps, H, d, generator=torch.Generator(device=DEV).manual_seed(7), device=DEV).half()
+        kc[:, page, at % block], vc[:, page, at % block] = own[0], own[1]
+        rows[name] = (kt, new)
+    torch.cuda.synchronize()
+    assert status[:7].tolist() == [0, 0, 0, 0, -1, 0, 0]
+    q = torch.randn(children, 2, Hq, d, generator=g).half()
+    results = {}
+    for name, (kt, new) in rows.items():
+        total = int(new[0].item())
+        prefix = (total - steps) // block * block
+        tiers = codec.tier if name == "full" else None
+        need = skv.attn_decode_workspace_size(children, 2, Hq, H, d, total, prefix)
+        aws = torch.empty(need, dtype=torch.uint8, device=DEV)
+        per = []
+        for layer in range(L):
+            out, lse = torch.empty_like(q, device=DEV), torch.empty(children, 2, Hq, device=DEV)
+            bad = torch.zeros(1, dtype=torch.int32, device=DEV)
+            skv.attn_decode(q.to(DEV), kc[layer], vc[layer], kt, new, out, aws, total, prefix_len=prefix, tiers=tiers,
+                            lse=lse, dev_status=bad)
+            assert bad.item() == 0
+            per.append((out, lse))
+            at = torch.arange(total, device=DEV)
+            want = []
+            for c in range(children):
+                r = (kt[c].long()[at // block], at % block)
+                seen = causal(2, total)
+                if tiers is not None:
+                    seen = seen & torch.cat([tiers != skv.DROP, torch.ones(steps, dtype=torch.bool, device=DEV)]).cpu()
+                want.append(attention(q[c], kc[layer][r].cpu(), vc[layer][r].cpu(), seen, d ** -0.5))
+            check(out, lse, tuple(torch.stack(x) for x in zip(*want)), (name, layer))
+        results[name] = per
+    for (a, al), (b, bl) in zip(results["full"], results["small"]):
+        # the same keys in other places: parts differ, values only by their roundings
+        assert (a.float() - b.float()).abs().max() <= 2 * 2.0 ** -11 * b.float().abs().max() + 2.0 ** -11 * 8
+        assert (al - bl).abs().max() < 1e-4
+    # everything released: the pool is as it was
+    for t, ln in [(tables, lens), (small, small_lens)] + list(rows.values()):
+        skv.pages_free(refs, t, ln, block, status[7:8])
+        assert status[7].item() == 0
+    assert torch.equal(refs, others)
+
+
+def test_cache_beyond_32_bits():
+    """Pages past 4 GiB of K: decode, fork and compact reach them."""
+    H, d, block = 8, 128, 16
+    nb = (1 << 32) // (block * H * d * 2) + 4000
+    kc, vc = (torch.empty(1, nb, block, H, d, dtype=torch.float16, device=DEV) for _ in range(2))
+    n, g = 300, torch.Generator().manual_seed(5)
+    pages = torch.arange(nb - 1, nb - 20, -1, dtype=torch.int32)
+    own = torch.randn(2, 19 * block, H, d, generator=g).half()
+    kc[0, pages.long().to(DEV)], vc[0, pages.long().to(DEV)] = (x.view(19, block, H, d).to(DEV) for x in own)
+    refs = torch.ones(nb, dtype=torch.int32, device=DEV)
+    refs[nb - 60:nb - 20] = 0
+    tables, lens = pages[None].to(DEV).contiguous(), torch.tensor([n], dtype=torch.int32, device=DEV)
+    tiers = torch.zeros(1, n, dtype=torch.uint8, device=DEV)
+    tiers[0, 1::3] = skv.DROP
+    ws = torch.empty(skv.pages_workspace_size(1, nb, 19 * block), dtype=torch.uint8, device=DEV)
+    small, small_lens, st = torch.zeros_like(tables), torch.zeros_like(lens), torch.zeros(2, dtype=torch.int32, device=DEV)
+    skv.pages_compact(kc, vc, refs, tables, lens, tiers, small, small_lens, ws, st[:1])
+    fork, fork_lens = torch.zeros_like(tables), torch.zeros_like(lens)
+    skv.pages_fork(kc, vc, refs, small, small_lens, torch.zeros_like(lens), fork, fork_lens, ws, st[1:])
+    assert st.tolist() == [0, 0] and small_lens.item() == 200 and fork_lens.item() == 200
+    q = torch.randn(1, 1, 8, d, generator=g).half()
+    kept = (tiers[0] != skv.DROP).cpu()
+    want = attention(q[0], own[0, :n][kept], own[1, :n][kept], torch.ones(1, 200, dtype=torch.bool), d ** -0.5)
+    want = tuple(x[None] for x in want)
+    for t, ln, m in ((tables, lens, tiers), (small, small_lens, None), (fork, fork_lens, None)):
+        out, lse = torch.empty_like(q, device=DEV), torch.empty(1, 1, 8, device=DEV)
+        aws = torch.empty(skv.attn_decode_workspace_size(1, 1, 8, H, d, n), dtype=torch.uint8, device=DEV)
+        skv.attn_decode(q.to(DEV), kc[0], vc[0], t, ln, out, aws, n, tiers=m, lse=lse)
+        check(out, lse, want)
+
+
+def test_pages_in_a_graph():
+    """A beam step captured once and replayed: fork, reserve, release; the pool is the same after each."""
+    L, nb, block, H, d, n = 2, 60, 16, 2, 64, 75
+    g = torch.Generator(device=DEV).manual_seed(2)
+    kc, vc = (torch.randn(L, nb, block, H, d, generator=g, device=DEV).half() for _ in range(2))
+    refs = torch.zeros(nb, dtype=torch.int32, device=DEV)
+    ws = torch.empty(skv.pages_workspace_size(4, nb, 6 * block), dtype=torch.uint8, device=DEV)
+    st = torch.full((4,), -1, dtype=torch.int32, device=DEV)
+    lens = torch.tensor([n], dtype=torch.int32, device=DEV)
+    tables = torch.zeros(1, 6, dtype=torch.int32, device=DEV)
+    skv.pages_reserve(refs, tables, torch.zeros_like(lens), lens, block, ws, st[:1])
+    held = refs.clone()
+    parents = torch.zeros(4, dtype=torch.int32, device=DEV)
+    kids, kid_lens = torch.zeros(4, 6, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    grown = kid_lens + n + 8
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        skv.pages_fork(kc, vc, refs, tables, lens, parents, kids, kid_lens, ws, st[1:2])
+        skv.pages_reserve(refs, kids, kid_lens, grown, block, ws, st[2:3])
+        skv.pages_free(refs, kids, grown, block, st[3:4])
+    for step in range(3):
+        kc[:, tables[0, 4].long(), :n - 64].normal_()
+        lens.fill_(n - step)
+        grown.fill_(n - step + 8)
+        kids.fill_(-1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert st.tolist() == [0, 0, 0, 0] and torch.equal(refs, held)
+        assert (kids[:, :4] == tables[:, :4]).all() and (kid_lens == n - step).all()
+        free = torch.nonzero(held == 0).flatten()
+        assert kids[:, 4].tolist() == free[:4].tolist()
+        m = n - step - 64
+        for c in range(4):
+            assert torch.equal(kc[:, kids[c, 4].long(), :m], kc[:, tables[0, 4].long(), :m])
+
+
+def test_no_requests():
+    """Calls with nothing to do."""
+    nb, block = 8, 16
+    kc = torch.zeros(1, nb, block, 2, 64, dtype=torch.float16, device=DEV)
+    refs, none = torch.zeros(nb, dtype=torch.int32, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV)
+    tables = torch.zeros(0, 3, dtype=torch.int32, device=DEV)
+    ws = torch.empty(skv.pages_workspace_size(0, nb, 48), dtype=torch.uint8, device=DEV)
+    st = torch.full((5,), -1, dtype=torch.int32, device=DEV)
+    skv.pages_reserve(refs, tables, none, none, block, ws, st[0:1])
+    skv.pages_fork(kc, kc, refs, tables, none, none, tables, none, ws, st[1:2])
+    skv.pages_compact(kc, kc, refs, tables, none, torch.zeros(0, 5, dtype=torch.uint8, device=DEV), tables, none, ws, st[2:3])
+    skv.pages_free(refs, tables, none, block, st[3:4])
+    skv.pages_copy(kc, kc, kc, kc, none, none, st[4:5])
+    assert st.tolist() == [0] * 5
+    q = torch.zeros(0, 4, 64, dtype=torch.float16, device=DEV)
+    skv.attn_prompt(q, kc[0, 0, :0], kc[0, 0, :0], q, [], [])
+    skv.attn_prompt(q, kc[0, 0, :0], kc[0, 0, :0], q, [0, 0], [0, 0])
+    skv.attn_decode(q[None][:0], kc[0], kc[0], tables, none, q[None][:0], None, 0)
+    torch.cuda.synchronize()
+
+
+def test_arguments_refused():
+    """What the binding checks on device tensors."""
+    q = torch.zeros(4, 4, 64, dtype=torch.float16, device=DEV)
+    k = torch.zeros(6, 2, 64, dtype=torch.float16, device=DEV)
+    out = torch.empty_like(q)
+
+    def refused(*a, error=(ValueError, TypeError, skv.SkvError), **kw):
+        with pytest.raises(error):
+            skv.attn_prompt(*a, **kw)
+
+    refused(q, k, k, out, [3], [6])
+    refused(q, k, k, out, [4], [5])
+    refused(q, k, k, out, [5, -1], [3, 3])
+    refused(q, k, k.bfloat16(), out)
+    refused(q, k, k[:5], out)
+    refused(q, k, k, out[:3])
+    refused(q, k, k, out.transpose(1, 2).contiguous().transpose(1, 2))
+    refused(q, k, [k], out)
+    refused(q, k, k, out, scale=-1.0)
+    refused(q, k, k, out, lse=torch.empty(3, 4, device=DEV))
+    refused(q[:, :3], k, k, out[:, :3])
+    refused(q.cpu(), k, k, out)
+    refused(q, k, k, out, ws=torch.empty(32, device=DEV))
+    cache, tables = torch.zeros(5, 16, 2, 64, dtype=torch.float16, device=DEV), torch.zeros(1, 2, dtype=torch.int32, device=DEV)
+    lens = torch.ones(1, dtype=torch.int32, device=DEV)
+    qd, od = q[:1, None], torch.empty_like(q[:1, None])
+    for change in (dict(tables=tables.long()), dict(tables=tables.T), dict(lens=lens[:0]), dict(k=cache[:4]),
+                   dict(k=cache.bfloat16(), v=cache.bfloat16()), dict(out=od[:, :, :3]), dict(prefix_len=8), dict(prefix_len=64),
+                   dict(tiers=torch.zeros(2, 3, dtype=torch.uint8, device=DEV)), dict(tiers=torch.zeros(3, device=DEV))):
+        a = dict(tables=tables, lens=lens, k=cache, v=cache, out=od)
+        kw = {x: change.pop(x) for x in ("prefix_len", "tiers") if x in change}
+        a.update(change)
+        with pytest.raises((ValueError, TypeError, skv.SkvError)):
+            skv.attn_decode(qd, a["k"], a["v"], a["tables"], a["lens"], a["out"], None, 20, **kw)
