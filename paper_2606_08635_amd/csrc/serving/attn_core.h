@@ -73,12 +73,13 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 
 // Direct global-to-LDS load: lane i's 16 bytes at src land at LDS byte address
 // lds_base + 16 i.  From inline assembly, so that the compiler does not count it
-// among its own loads; the tile loop waits for it itself (wait_direct_loads).
+// among its own loads; the tile loop waits for it itself (wait_direct_loads).  A
+// load that reads m0 needs one wait state behind the write of it: the s_nop.
 __device__ __forceinline__ void direct_load(const void* src, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds_base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds_base) : "memory", "m0");
 }
 __device__ __forceinline__ void direct_load(const void* uniform_base, uint32_t offset, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(uniform_base), "s"(lds_base)
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(uniform_base), "s"(lds_base)
                : "memory", "m0");
 }
 __device__ __forceinline__ void wait_direct_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
