@@ -555,7 +555,9 @@ skv_status skv_link(void* dst, const void* src, uint64_t bytes, void* host_stagi
  * -infinity.  Query head hq reads KV head hq / (Hq / H).  Products are exact,
  * sums binary32, probabilities rounded to the 16-bit type before their product
  * with V, results rounded once.  NaN and infinities follow IEEE softmax over the
- * visible keys; hidden keys' K and V, whatever they hold, have no effect.
+ * visible keys (but a key whose probability underflows to 0 has no effect, where
+ * IEEE's 0 times infinity is NaN); hidden keys' K and V, whatever they hold, have
+ * no effect.
  * Results of a call are the same every time. */
 enum { SKV_DTYPE_F16 = 0, SKV_DTYPE_BF16 = 1 };
 
@@ -613,9 +615,11 @@ typedef struct skv_decode_config {
   int32_t num_queries;   /* Lq: newest tokens of each request, already in the
                             cache (1; more to verify drafted tokens; 0: nothing
                             to do)                                                */
-  int32_t num_q_heads, num_kv_heads, head_dim; /* as skv_attn_config              */
+  int32_t num_q_heads, num_kv_heads, head_dim; /* as skv_attn_config;
+                            B Lq <= 2^20, B Lq Hq < 2^26                          */
   int32_t num_blocks, block_size;              /* num_blocks * block_size < 2^31  */
-  int32_t table_width;   /* entries of a request's block table                    */
+  int32_t table_width;   /* entries of a request's block table; times block_size
+                            at most 2^30                                          */
   int32_t max_len;       /* about the longest request's tokens: sizes the launch;
                             any request may be shorter or longer                  */
   int32_t prefix_len;    /* tokens at the start of every request that are the same
@@ -668,9 +672,10 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
  * when too few pages are free or an output table is too narrow.  With a status
  * other than 0 a call has changed nothing else (skv_pages_free excepted, see
  * there).  ws: skv_pages_workspace_size bytes (ws_bytes; SKV_ERR_CAPACITY if less).
- * Calls on one pool, and calls that share ws, must be ordered on one stream.
- * Alignment 16 (k_cache, v_cache, refs, ws), 4 (int32 arrays, dev_status).  Kernel
- * launches only: the calls can be captured in a HIP graph. */
+ * Calls on one pool, and calls that share ws or dev_status, must be ordered on one
+ * stream.  At most 2^24 requests; width * block_size at most 2^30.  Alignment 16
+ * (k_cache, v_cache, refs, ws), 4 (int32 arrays, dev_status).  Kernel launches
+ * only: the calls can be captured in a HIP graph. */
 typedef struct skv_page_pool {
   int32_t num_layers;  /* L                                                       */
   int32_t num_blocks;  /* num_blocks * block_size < 2^31                           */
@@ -696,7 +701,8 @@ skv_status skv_pages_reserve(const skv_page_pool* pool, int32_t* tables, int32_t
  * children).  Its full pages are shared (their counts go up by one per child); of
  * a partly filled last page the child gets a page of its own, with the filled rows
  * copied in every layer.  out_tables [num_children][out_width], out_lens
- * int32[num_children]; they may not overlap tables and lens. */
+ * int32[num_children]; neither may overlap the other, tables, lens or parents
+ * (SKV_ERR_INVALID_ARG). */
 skv_status skv_pages_fork(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
                           int32_t num_requests, const int32_t* parents, int32_t num_children, int32_t* out_tables,
                           int32_t out_width, int32_t* out_lens, uint32_t* dev_status, void* ws, uint64_t ws_bytes,
@@ -708,7 +714,8 @@ skv_status skv_pages_fork(const skv_page_pool* pool, const int32_t* tables, int3
  * token are shared as in a fork, the rows behind are gathered into new pages in
  * every layer.  The source keeps its pages until skv_pages_free.  Positions change:
  * a cold-tier upgrade names tokens by their old ones and belongs before.  The
- * tables serve every layer and head, so one map per request. */
+ * tables serve every layer and head, so one map per request.  out_tables and
+ * out_lens as in skv_pages_fork. */
 skv_status skv_pages_compact(const skv_page_pool* pool, const int32_t* tables, int32_t table_width, const int32_t* lens,
                              int32_t num_requests, const uint8_t* tiers, int32_t tier_len, int64_t tier_stride,
                              int32_t* out_tables, int32_t out_width, int32_t* out_lens, uint32_t* dev_status, void* ws,

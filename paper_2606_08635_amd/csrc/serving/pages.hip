@@ -355,7 +355,8 @@ __global__ __launch_bounds__(kPlanThreads) void pages_free(const PageArgs a, int
     if (threadIdx.x == 0) *a.status = SKV_OK;
     __syncthreads();
   }
-  const uint32_t all = static_cast<uint32_t>(a.rows) * static_cast<uint32_t>(a.width), step = gridDim.x * kPlanThreads;
+  const uint32_t width = static_cast<uint32_t>(max(1, a.width));  // (with none the lengths are still looked at)
+  const uint32_t all = static_cast<uint32_t>(a.rows) * width, step = gridDim.x * kPlanThreads;
   bool bad = false;
   for (uint64_t e0 = blockIdx.x * kPlanThreads + threadIdx.x; e0 < all; e0 += 4 * static_cast<uint64_t>(step)) {
     int n[4], page[4];
@@ -366,9 +367,9 @@ __global__ __launch_bounds__(kPlanThreads) void pages_free(const PageArgs a, int
       n[i] = 0;
       if (e >= all) continue;
       const uint32_t b = a.by_width.div(static_cast<uint32_t>(e));
-      j[i] = static_cast<uint32_t>(e) - b * static_cast<uint32_t>(a.width);
+      j[i] = static_cast<uint32_t>(e) - b * width;
       n[i] = a.lens[b];
-      page[i] = a.tables[e];
+      page[i] = a.width > 0 ? a.tables[e] : -1;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -408,8 +409,13 @@ __global__ __launch_bounds__(256) void pages_copy(const PageCopyArgs a, uint32_t
   for (uint64_t unit = u0; unit < min(u0 + kUnits, a.units); ++unit) {
     const uint32_t at = static_cast<uint32_t>(unit / a.pieces), piece = static_cast<uint32_t>(unit % a.pieces);
     const uint32_t plane = at % a.planes, pair = at / a.planes;
-    const int64_t from = static_cast<int64_t>(plane >> 1) * a.src_plane_bytes + a.src_pages[pair] * a.page_bytes;
-    const int64_t to = static_cast<int64_t>(plane >> 1) * a.dst_plane_bytes + a.dst_pages[pair] * a.page_bytes;
+    const int32_t src_page = a.src_pages[pair], dst_page = a.dst_pages[pair];
+    // (checked: passed over here only where the status was written by another call meanwhile)
+    if (static_cast<uint32_t>(src_page) >= static_cast<uint32_t>(a.src_blocks) ||
+        static_cast<uint32_t>(dst_page) >= static_cast<uint32_t>(a.dst_blocks))
+      continue;
+    const int64_t from = static_cast<int64_t>(plane >> 1) * a.src_plane_bytes + src_page * a.page_bytes;
+    const int64_t to = static_cast<int64_t>(plane >> 1) * a.dst_plane_bytes + dst_page * a.page_bytes;
     const uint8_t* src = (plane & 1 ? a.src_v : a.src_k) + from;
     uint8_t* dst = (plane & 1 ? a.dst_v : a.dst_k) + to;
     const int64_t end = min(a.page_bytes, static_cast<int64_t>(piece + 1) * kPiece);
@@ -447,7 +453,7 @@ hipError_t launch_pages(const PageArgs& a, hipStream_t stream) {
 hipError_t launch_pages_free(const PageArgs& a, hipStream_t stream) {
   // one workgroup clears the status itself (2000 entries: 3 us); more need it cleared
   // before any of them starts
-  const uint64_t all = static_cast<uint64_t>(a.rows) * a.width;
+  const uint64_t all = static_cast<uint64_t>(a.rows) * std::max(1, a.width);
   const uint32_t groups = all <= 8 * kPlanThreads ? 1 : static_cast<uint32_t>(std::min<uint64_t>((all + 4095) / 4096, 256));
   if (groups > 1) {
     pages_clear_status<<<1, 1, 0, stream>>>(a.status);

@@ -3,8 +3,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <numeric>
-#include <vector>
 
 #include "serving_internal.h"
 
@@ -53,11 +51,20 @@ skv_status check_prompt(const skv_attn_config* c, const skv_attn_request* reqs, 
 // 32-row tiles of a workgroup for this many rows.
 int32_t row_tiles(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
-// How a launch of requests [0, n) (already ordered) runs.
+// The requests of a launch, longest first (the heaviest workgroups start first).
+struct PromptBatch {
+  const skv_attn_request* r[kMaxPromptBatch];
+  int32_t n;
+  const skv_attn_request* const* begin() const { return r; }
+  const skv_attn_request* const* end() const { return r + n; }
+};
+
+// How a launch runs.
 struct PromptPlan {
   int32_t key_streams, row_tiles;
-  std::vector<int32_t> splits;
-  uint64_t rows;  // partial rows
+  int32_t splits[kMaxPromptBatch];
+  uint64_t rows;    // partial rows
+  uint64_t blocks;  // workgroups of an unsplit launch
 };
 
 int64_t prompt_blocks(const skv_attn_config* c, const skv_attn_request& r, int32_t per) {
@@ -65,8 +72,8 @@ int64_t prompt_blocks(const skv_attn_config* c, const skv_attn_request& r, int32
   return (rows + per - 1) / per * c->num_kv_heads;
 }
 
-PromptPlan plan_prompt(const skv_attn_config* c, const std::vector<const skv_attn_request*>& reqs) {
-  PromptPlan p{1, 4, {}, 0};
+PromptPlan plan_prompt(const skv_attn_config* c, const PromptBatch& reqs) {
+  PromptPlan p{1, 4, {}, 0, 0};
   const int64_t room = c->head_dim >= 256 ? kCus : 2 * kCus;  // workgroups that the GPU holds at once
   auto blocks = [&](int32_t tiles) {
     int64_t n = 0;
@@ -91,32 +98,30 @@ PromptPlan plan_prompt(const skv_attn_config* c, const std::vector<const skv_att
   // keys: 474 us in one part, 77 in 16); a second launch and its traffic cost about
   // 10 us, so short keys are left whole.
   const int64_t all = std::max<int64_t>(1, blocks(p.row_tiles));
-  for (const skv_attn_request* r : reqs) {
-    const int64_t rows = static_cast<int64_t>(r->num_queries) * c->num_q_heads;
+  p.blocks = static_cast<uint64_t>(all);
+  for (int32_t i = 0; i < reqs.n; ++i) {
+    const int64_t rows = static_cast<int64_t>(reqs.r[i]->num_queries) * c->num_q_heads;
     int64_t s = 1;
-    if (splits && 2 * all <= room) s = std::max<int64_t>(1, std::min<int64_t>({room / all, r->num_keys / 256, 64}));
-    p.splits.push_back(static_cast<int32_t>(s));
+    if (splits && 2 * all <= room) s = std::max<int64_t>(1, std::min<int64_t>({room / all, reqs.r[i]->num_keys / 256, 64}));
+    p.splits[i] = static_cast<int32_t>(s);
     if (s > 1) p.rows += static_cast<uint64_t>(rows * s);
   }
   return p;
 }
 
-// The requests with queries, longest first (the heaviest workgroups start first).
-std::vector<const skv_attn_request*> prompt_order(const skv_attn_request* reqs, int32_t count) {
-  std::vector<const skv_attn_request*> order;
-  for (int32_t i = 0; i < count; ++i)
-    if (reqs[i].num_queries > 0) order.push_back(&reqs[i]);
-  std::stable_sort(order.begin(), order.end(),
-                   [](const skv_attn_request* x, const skv_attn_request* y) { return x->num_keys > y->num_keys; });
-  return order;
-}
-
+// The launches of a call: its requests with queries in their order, kMaxPromptBatch
+// at a time, sorted within one.  Nothing here allocates.
 template <class F>
 skv_status prompt_launches(const skv_attn_config* c, const skv_attn_request* reqs, int32_t count, F each) {
-  const std::vector<const skv_attn_request*> order = prompt_order(reqs, count);
-  for (size_t first = 0; first < order.size(); first += kMaxPromptBatch) {
-    const size_t n = std::min<size_t>(kMaxPromptBatch, order.size() - first);
-    const std::vector<const skv_attn_request*> some(order.begin() + first, order.begin() + first + n);
+  for (int32_t at = 0; at < count;) {
+    PromptBatch some;
+    for (some.n = 0; at < count && some.n < kMaxPromptBatch; ++at) {
+      if (reqs[at].num_queries == 0) continue;
+      int32_t i = some.n++;
+      for (; i > 0 && some.r[i - 1]->num_keys < reqs[at].num_keys; --i) some.r[i] = some.r[i - 1];
+      some.r[i] = &reqs[at];
+    }
+    if (some.n == 0) break;
     const skv_status st = each(some, plan_prompt(c, some));
     if (st != SKV_OK) return st;
   }
@@ -175,7 +180,7 @@ skv_status check_decode_sizes(const skv_decode_config* c) {
     return SKV_ERR_INVALID_ARG;
   if (c->num_requests < 0 || c->num_queries < 0 || c->max_len < 0 || c->prefix_len < 0) return SKV_ERR_INVALID_ARG;
   if (static_cast<int64_t>(c->num_requests) * c->num_queries > (1 << 20) ||
-      static_cast<int64_t>(c->num_requests) * c->num_queries * c->num_q_heads > (1 << 26))
+      static_cast<int64_t>(c->num_requests) * c->num_queries * c->num_q_heads >= (1 << 26))
     return SKV_ERR_INVALID_ARG;
   return SKV_OK;
 }
@@ -203,7 +208,7 @@ bool pool_ok(const skv_page_pool* p, bool caches, bool refs) {
 }
 
 bool tables_ok(const skv_page_pool* p, const void* tables, int32_t width, const void* lens, int32_t requests) {
-  if (requests < 0 || width < 0 || static_cast<int64_t>(width) * p->block_size > (1 << 30) ||
+  if (requests < 0 || requests > (1 << 24) || width < 0 || static_cast<int64_t>(width) * p->block_size > (1 << 30) ||
       static_cast<int64_t>(requests) * width > INT32_MAX)
     return false;
   return requests == 0 || (aligned(lens, 4) && (width == 0 || aligned(tables, 4)));
@@ -254,13 +259,33 @@ skv_status page_workspace(PageArgs* a, int64_t chunks, void* ws, uint64_t ws_byt
   return SKV_OK;
 }
 
+// Whether an output of fork or compact lies on one of their inputs, which the last
+// launch still reads.
+struct Span {
+  const void* p;
+  uint64_t n;  // int32 entries
+};
+bool overlap(const Span& x, const Span& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  return x.n > 0 && y.n > 0 && a < b + 4 * y.n && b < a + 4 * x.n;
+}
+bool outputs_apart(const PageArgs& a) {
+  const uint64_t rows = static_cast<uint64_t>(a.rows), sources = static_cast<uint64_t>(a.sources);
+  const Span in[3] = {{a.tables, sources * static_cast<uint64_t>(a.width)}, {a.lens, sources}, {a.parents, a.parents ? rows : 0}};
+  const Span out[2] = {{a.out_tables, rows * static_cast<uint64_t>(a.out_width)}, {a.out_lens, rows}};
+  bool apart = !overlap(out[0], out[1]);
+  for (const Span& x : in) apart = apart && !overlap(x, out[0]) && !overlap(x, out[1]);
+  return apart;
+}
+
 // Workgroups of the row copies: the planes are spread until the launch has about
 // `want` workgroups.
 skv_status spread_planes(PageArgs* a, int64_t pieces, int64_t want) {
   const int64_t planes = 2 * static_cast<int64_t>(a->num_layers);
   a->plane_groups = static_cast<int32_t>(std::max<int64_t>(1, std::min(planes, (want + pieces - 1) / pieces)));
   const int64_t groups = pieces * a->plane_groups;
-  if (groups > static_cast<int64_t>(kMaxGridThreads / 256)) return SKV_ERR_CAPACITY;
+  // (a table's entries, at most 2^31, take 2^21 workgroups more)
+  if (groups > static_cast<int64_t>(kMaxGridThreads / 512)) return SKV_ERR_CAPACITY;
   a->copy_groups = static_cast<uint32_t>(groups);
   return SKV_OK;
 }
@@ -278,7 +303,7 @@ skv_status skv_attn_prompt_workspace_size(const skv_attn_config* cfg, const skv_
   const skv_status st = check_prompt(cfg, reqs, count, false);
   if (st != SKV_OK) return st;
   uint64_t most = 0;
-  prompt_launches(cfg, reqs, count, [&](const std::vector<const skv_attn_request*>&, const PromptPlan& p) {
+  prompt_launches(cfg, reqs, count, [&](const PromptBatch&, const PromptPlan& p) {
     most = std::max(most, p.rows * static_cast<uint64_t>(cfg->head_dim + 2) * 4u);
     return SKV_OK;
   });
@@ -288,13 +313,18 @@ skv_status skv_attn_prompt_workspace_size(const skv_attn_config* cfg, const skv_
 
 skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* reqs, int32_t count, void* ws,
                            uint64_t ws_bytes, hipStream_t stream) {
-  const skv_status st = check_prompt(cfg, reqs, count, true);
+  skv_status st = check_prompt(cfg, reqs, count, true);
   if (st != SKV_OK) return st;
   if (ws != nullptr && !aligned(ws, 16)) return SKV_ERR_INVALID_ARG;
-  return prompt_launches(cfg, reqs, count, [&](const std::vector<const skv_attn_request*>& some, const PromptPlan& p) {
+  // (split launches are small ones: this bounds them too)
+  st = prompt_launches(cfg, reqs, count, [](const PromptBatch&, const PromptPlan& p) {
+    return p.blocks > kMaxGridThreads / 512 ? SKV_ERR_CAPACITY : SKV_OK;
+  });
+  if (st != SKV_OK) return st;
+  return prompt_launches(cfg, reqs, count, [&](const PromptBatch& some, const PromptPlan& p) {
     PromptArgs a;
     std::memset(&a, 0, sizeof(a));
-    a.count = static_cast<int32_t>(some.size());
+    a.count = some.n;
     a.H = cfg->num_kv_heads;
     a.G = cfg->num_q_heads / cfg->num_kv_heads;
     a.causal = cfg->causal;
@@ -310,7 +340,7 @@ skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* r
     a.part_ml = split ? a.part_o + p.rows * static_cast<uint64_t>(cfg->head_dim) : nullptr;
     uint64_t begin = 0, rows_at = 0;
     for (int32_t i = 0; i < a.count; ++i) {
-      const skv_attn_request& q = *some[i];
+      const skv_attn_request& q = *some.r[i];
       PromptDesc& r = a.r[i];
       r.q = static_cast<const uint16_t*>(q.q);
       r.k = static_cast<const uint16_t*>(q.k);
@@ -326,7 +356,6 @@ skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* r
       r.rows_at = static_cast<uint32_t>(rows_at);
       begin += static_cast<uint64_t>(prompt_blocks(cfg, q, 32 * a.row_tiles)) * static_cast<uint64_t>(r.splits);
       if (r.splits > 1) rows_at += static_cast<uint64_t>(q.num_queries) * cfg->num_q_heads * r.splits;
-      if (begin > kMaxGridThreads / 256 || rows_at > UINT32_MAX) return SKV_ERR_CAPACITY;
     }
     a.blocks = static_cast<uint32_t>(begin);
     return launch_attn_prompt(a, cfg->dtype, cfg->head_dim, stream) == hipSuccess ? SKV_OK : SKV_ERR_DEVICE;
@@ -348,7 +377,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   const skv_decode_config& c = *cfg;
   if (!shape_ok(c.dtype, c.num_q_heads, c.num_kv_heads, c.head_dim, c.scale)) return SKV_ERR_INVALID_ARG;
   if (c.num_blocks < 1 || c.block_size < 1 || static_cast<int64_t>(c.num_blocks) * c.block_size > INT32_MAX ||
-      c.table_width < 0 || static_cast<int64_t>(c.table_width) * c.block_size > INT32_MAX - 2 * 1024 ||
+      c.table_width < 0 || static_cast<int64_t>(c.table_width) * c.block_size > (1 << 30) ||
       c.table_stride < c.table_width)
     return SKV_ERR_INVALID_ARG;
   if (c.prefix_len % c.block_size != 0 || c.prefix_len > c.table_width * c.block_size) return SKV_ERR_INVALID_ARG;
@@ -362,7 +391,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
     return SKV_ERR_INVALID_ARG;
   const DecodePlan p = plan_decode(cfg);
   if (p.bytes > 0 && !aligned(ws, 16)) return SKV_ERR_INVALID_ARG;
-  if (ws_bytes < p.bytes || p.groups > kMaxGridThreads / 256) return SKV_ERR_CAPACITY;
+  if (ws_bytes < p.bytes || p.groups > kMaxGridThreads / 512) return SKV_ERR_CAPACITY;
   const int32_t H = c.num_kv_heads, G = c.num_q_heads / H;
   DecodeArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -458,6 +487,7 @@ skv_status skv_pages_fork(const skv_page_pool* pool, const int32_t* tables, int3
   // one workgroup looks over 16384 entries in about 5 us, less than a launch more costs
   a.checked = static_cast<int64_t>(num_children) * table_width > 16384;
   skv_status st = page_workspace(&a, 0, ws, ws_bytes);
+  if (st == SKV_OK && !outputs_apart(a)) st = SKV_ERR_INVALID_ARG;
   if (st == SKV_OK) st = spread_planes(&a, std::max(1, num_children), 1024);
   if (st != SKV_OK) return st;
   if (num_children == 0) a.copy_groups = 0;
@@ -482,6 +512,7 @@ skv_status skv_pages_compact(const skv_page_pool* pool, const int32_t* tables, i
   a.out_lens = out_lens;
   a.chunks = static_cast<int32_t>(std::max<int64_t>(1, (static_cast<int64_t>(table_width) * pool->block_size + 255) / 256));
   skv_status st = page_workspace(&a, a.chunks, ws, ws_bytes);
+  if (st == SKV_OK && !outputs_apart(a)) st = SKV_ERR_INVALID_ARG;
   if (st == SKV_OK) st = spread_planes(&a, std::max<int64_t>(1, static_cast<int64_t>(num_requests) * a.chunks), 4096);
   if (st != SKV_OK) return st;
   if (num_requests == 0) a.copy_groups = 0;

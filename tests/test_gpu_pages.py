@@ -250,3 +250,12 @@ def test_free_passes_over_what_is_not_held():
     p.refs[tables[1, 0]] -= 1
     p.check()
     assert st.item() == skv.ERR_FORMAT and (p.refs == 0).all()
+
+
+def test_free_without_entries():
+    """Tables of no width: requests of no tokens hold nothing, a longer one is reported."""
+    refs, st = torch.ones(8, dtype=torch.int32, device=DEV), torch.full((2,), -1, dtype=torch.int32, device=DEV)
+    tables = torch.zeros(3, 0, dtype=torch.int32, device=DEV)
+    skv.pages_free(refs, tables, torch.zeros(3, dtype=torch.int32, device=DEV), 16, st[:1])
+    skv.pages_free(refs, tables, torch.tensor([0, 5, 0], dtype=torch.int32, device=DEV), 16, st[1:])
+    assert st.tolist() == [skv.OK, skv.ERR_FORMAT] and (refs == 1).all()

@@ -193,3 +193,31 @@ def test_host_tensors_refused():
         skv.attn_decode(x[None], c, c, t, t[0], x[None], None, 4)
     with pytest.raises(ValueError):
         skv.pages_free(t[0], t, t[0], 16, t[0])
+
+
+def test_sizes_past_the_limits_refused(lib):
+    """Just past what a launch and the kernels' indexes hold: refused by the host."""
+    assert _decode(lib, B=1 << 10, Lq=1 << 10, Hq=64, H=64) == BAD
+    assert _decode(lib, width=(1 << 26) + 1, ts=(1 << 26) + 1) == BAD
+    # 48 small requests and one that no grid holds: nothing of it is launched
+    cfg = skv._ATTN_CONFIG.pack(0, 4096, 4096, 32, 1, 0.1, 1 << 17, 32, 1 << 17, 32)
+    small, huge = (skv._ATTN_REQUEST.pack(n, n, P, P, P, P, 0, 1 << 17, 32) for n in (1, 1 << 20))
+    assert lib.skv_attn_prompt(cfg, small * 48 + huge, 49, None, 0, None) == skv.ERR_CAPACITY
+    p, ws = _pool(), 1 << 40
+    assert lib.skv_pages_free(p, P, 0, P, (1 << 24) + 1, P, None) == BAD
+    assert lib.skv_pages_reserve(p, P, 0, P, P, (1 << 24) + 1, P, P, ws, None) == BAD
+
+
+@pytest.mark.parametrize("out,out_lens,fork_only", [
+    (0x10000, 0x90000, False),         # the tables themselves
+    (0x10000 + 20, 0x90000, False),    # their last entry
+    (0x80000, 0x20000, False),         # the lengths themselves
+    (0x20000 - 8, 0x90000, False), (0x80000, 0x10008, False), (0x80000, 0x80000 + 8, False),
+    (0x30000, 0x90000, True), (0x80000, 0x30000, True)])  # the parents
+def test_outputs_on_inputs_refused(lib, out, out_lens, fork_only):
+    """Fork and compact read their inputs until their last launch."""
+    p, ws = _pool(), 1 << 20
+    tables, lens, parents = 0x10000, 0x20000, 0x30000
+    assert lib.skv_pages_fork(p, tables, 3, lens, 2, parents, 2, out, 3, out_lens, P, P, ws, None) == BAD
+    if not fork_only:
+        assert lib.skv_pages_compact(p, tables, 3, lens, 2, P, 12, 12, out, 3, out_lens, P, P, ws, None) == BAD
