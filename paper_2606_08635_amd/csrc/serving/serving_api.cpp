@@ -144,14 +144,19 @@ DecodePlan plan_decode(const skv_decode_config* c) {
   auto up = [](int64_t x, int64_t to) { return (x + to - 1) / to; };
   p.tail_tiles = row_tiles(own);
   p.tail_blocks = static_cast<int32_t>(up(own, 32 * p.tail_tiles));
-  // The prefix gets half the room (a quarter at D = 256, where a compute unit holds one
-  // workgroup), in parts of at least 128 tokens: more parts are more partial results
-  // to write and join (64 requests behind 16384 tokens of 8 x 128: 51 us with 512
-  // workgroups, 41 with 256, 47 with 128).
+  // The prefix gets the share of the room that its tiles are of all (one of many rows
+  // counted twice, the tails taken to be half as long as the longest), at most half:
+  // more parts are more partial results to write and join (64 requests behind 16384
+  // tokens of 8 x 128: 47 us with 512 workgroups, 40 with 256, 47 with 128).  By its
+  // share against always half: 64 behind 2048 with up to 3800 of their own, 123 us
+  // against 139; 12 behind 2048 of 8 x 256, 5 queries each, with up to 1450, 34
+  // against 47.
   if (c->prefix_len > 0) {
     p.prefix_tiles = row_tiles(all);
     p.prefix_blocks = static_cast<int32_t>(up(all, 32 * p.prefix_tiles));
-    const int64_t share = c->head_dim >= 256 ? room / 4 : room / 2;
+    const int64_t here = 2 * p.prefix_blocks * up(c->prefix_len, 64);
+    const int64_t there = c->num_requests * p.tail_blocks * up(tail / 2, 64);
+    const int64_t share = std::min(room / 2, room * here / (here + there));
     const int64_t parts = std::max<int64_t>(1, std::min(share / (H * p.prefix_blocks), up(c->prefix_len, 128)));
     p.prefix_chunk = static_cast<int32_t>(up(up(c->prefix_len, parts), 64) * 64);
     p.prefix_parts = static_cast<int32_t>(up(c->prefix_len, p.prefix_chunk));
