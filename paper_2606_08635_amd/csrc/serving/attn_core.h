@@ -305,6 +305,8 @@ struct WaveAttention {
     const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, top * alpha));
     return fmaxf(__builtin_bit_cast(float, p.lo), __builtin_bit_cast(float, p.hi));
   }
+  // Whether no row has a reference yet: the first step takes the maximum at once.
+  __device__ __forceinline__ bool fresh() const { return __all(m == -INFINITY); }
   // Raises m to mn >= m; returns the value to exponentiate against (0 while nothing
   // has been seen, so that every probability is 0).
   __device__ __forceinline__ float raise(float mn) {
@@ -423,7 +425,8 @@ struct WaveAttention {
           if (!visible(n, r)) x[n][r] = -INFINITY;
     }
     float e[NS][16];
-    float sum = exponentials(x, alpha, m, e);
+    float sum = INFINITY;
+    if (__builtin_expect(!fresh(), 1)) sum = exponentials(x, alpha, m, e);
     if (__builtin_expect(__any(!(sum <= kHigh)), 0)) sum = exponentials(x, alpha, raise(fmaxf(m, largest(x, alpha))), e);
     l += sum;
     u32x4 p[2 * NS], rest[2 * NS];

@@ -198,30 +198,35 @@ __device__ __forceinline__ Place place(uint32_t i, uint32_t runs, uint32_t block
   return p;
 }
 
-// Where a tail workgroup's part lies: request and tiles of its tail.
+// Where a tail workgroup's part lies: request, and tokens of its tail.
 struct TailPart {
   int request, first, last;
 };
 __device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
   return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_inclusive_scan(x)), 63));
 }
-// Cuts the tails into parts of c tiles, c the smallest (from 2 on) that gives at most
-// a.tail_parts parts, and finds part `at`; false past the last.  Every wave does it
-// for itself, a lane holding four requests, so nothing waits for another wave.
-// `tell`: write the requests' first parts and counts for the join.
+// Cuts the tails into parts of c tiles, c the smallest (from a.tail_least on) that
+// gives at most a.tail_parts parts, and finds part `at`; false past the last.  (With
+// N tiles of B requests, c >= N / parts, and c >= N / (parts - B) always gives few
+// enough.)  Every wave does it for itself, a lane holding four requests, so nothing
+// waits for another wave.  `tell`: write the requests' first parts and counts for
+// the join.
 __device__ __forceinline__ bool find_part(const DecodeArgs& a, int at, bool tell, TailPart& part) {
   const int lane = threadIdx.x & 63;
-  uint32_t n[4], all = 0, most = 0;
+  uint32_t tokens[4], n[4], all = 0, most = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    n[i] = 4 * lane + i < a.B ? static_cast<uint32_t>(tail_tokens(a, 4 * lane + i) + 63) / 64 : 0;
+    tokens[i] = 4 * lane + i < a.B ? static_cast<uint32_t>(tail_tokens(a, 4 * lane + i)) : 0;
+    n[i] = (tokens[i] + 63) / 64;
     all += n[i];
     most = max(most, n[i]);
   }
   all = wave_sum(all);
   most = wave_max(most);
   const uint32_t limit = static_cast<uint32_t>(a.tail_parts);
-  uint32_t lo = max(2u, (all + limit - 1) / limit), hi = max(lo, most);  // hi gives one part per request
+  uint32_t lo = max(static_cast<uint32_t>(a.tail_least), (all + limit - 1) / limit), hi = max(lo, most);  // (most: one part per request)
+  const uint32_t spare = limit - static_cast<uint32_t>(a.B);
+  if (spare > 0) hi = min(hi, max(lo, (all + spare - 1) / spare));
   while (lo < hi) {
     const uint32_t c = (lo + hi) >> 1;
     uint32_t parts = 0;
@@ -238,14 +243,14 @@ __device__ __forceinline__ bool find_part(const DecodeArgs& a, int at, bool tell
   }
   uint32_t begin = wave_inclusive_scan(mine) - mine;
   int request = -1;
-  uint32_t first = 0, tiles = 0;
+  uint32_t first = 0, end = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t u = static_cast<uint32_t>(at) - begin;  // (wraps where the part lies before)
     if (u < count[i]) {
       request = 4 * lane + i;
-      first = u * lo;
-      tiles = n[i];
+      first = 64 * u * lo;
+      end = tokens[i];
     }
     if (tell && 4 * lane + i < a.B) {
       a.first_part[4 * lane + i] = static_cast<int32_t>(begin);
@@ -258,7 +263,7 @@ __device__ __forceinline__ bool find_part(const DecodeArgs& a, int at, bool tell
   const int from = __builtin_ctzll(has);
   part.request = __builtin_amdgcn_readlane(request, from);
   part.first = __builtin_amdgcn_readlane(static_cast<int>(first), from);
-  part.last = min(part.first + static_cast<int>(lo), __builtin_amdgcn_readlane(static_cast<int>(tiles), from));
+  part.last = min(part.first + static_cast<int>(64 * lo), __builtin_amdgcn_readlane(static_cast<int>(end), from));
   return true;
 }
 
@@ -294,8 +299,8 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
       TailPart part;
       if (!find_part(a, static_cast<int>(p.run), blockIdx.x == a.prefix_groups && threadIdx.x < 64, part)) return;
       b = part.request;
-      p1 = a.prefix + min(tail_tokens(a, b), 64 * part.last);
-      p0 += 64 * part.first;
+      p1 = a.prefix + part.last;
+      p0 += part.first;
     }
     row0 = b * own + static_cast<int>(p.blk) * tiles * 32;
     rows = min(tiles * 32, own - static_cast<int>(p.blk) * tiles * 32);

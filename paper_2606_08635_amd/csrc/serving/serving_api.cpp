@@ -131,7 +131,7 @@ skv_status prompt_launches(const skv_attn_config* c, const skv_attn_request* req
 // How skv_attn_decode cuts its work (the counts, lengths and dimensions of c are
 // valid).
 struct DecodePlan {
-  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, tail_parts, tail_blocks, tail_tiles;
+  int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk, tail_parts, tail_blocks, tail_tiles, tail_least;
   uint64_t prefix_groups, groups, prefix_rows, part_rows, bytes;  // (bytes 0: no parts)
 };
 
@@ -164,12 +164,16 @@ DecodePlan plan_decode(const skv_decode_config* c) {
     p.prefix_rows = static_cast<uint64_t>(p.prefix_parts * H * all);
   }
   // The tails in as many parts as fill the rest of the room, two per request at least
-  // where they may be long and uneven, and not more than 128 tokens each would give
-  // (as far as max_len says); whole where that fills the room with short ones (64
-  // requests of up to 400 tokens: 14 us whole, 20 with a second launch for the parts).
+  // where they may be long and uneven, of 128 tokens at least (as far as max_len says);
+  // of 64 where so few fill at most half the room and a request has 32 at most, which
+  // its join reads at once (one request of 500 tokens of 8 x 128: 11.9 us against
+  // 12.8; of 8192 of 4 x 128: 16.6 against 14.4); whole where that fills the room with
+  // short ones (64 requests of up to 400 tokens: 14 us whole, 20 with a second launch
+  // for the parts).
   const int64_t groups = H * p.tail_blocks, left = room - static_cast<int64_t>(p.prefix_groups);
+  p.tail_least = tail <= 2048 && 2 * groups * c->num_requests * up(tail, 64) <= room ? 1 : 2;
   int64_t parts = std::max(left / groups, c->num_requests * static_cast<int64_t>(tail >= 2048 ? 2 : 1));
-  parts = std::min(parts, c->num_requests * up(tail, 128));
+  parts = std::min(parts, c->num_requests * up(tail, 64 * p.tail_least));
   const bool whole = tail <= 256 || (tail < 2048 && c->num_requests * groups >= left);
   if (c->num_requests <= kCutRequests && !whole && parts > 1) p.tail_parts = static_cast<int32_t>(parts);
   const int64_t runs = p.tail_parts > 0 ? p.tail_parts : c->num_requests;
@@ -343,6 +347,9 @@ skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* r
     const bool split = ws != nullptr && ws_bytes >= p.rows * static_cast<uint64_t>(cfg->head_dim + 2) * 4u;
     a.part_o = static_cast<float*>(ws);
     a.part_ml = split ? a.part_o + p.rows * static_cast<uint64_t>(cfg->head_dim) : nullptr;
+    a.by_H = make_divider(static_cast<uint32_t>(a.H));
+    a.by_G = make_divider(static_cast<uint32_t>(a.G));
+    std::fill(a.begin, a.begin + kMaxPromptBatch, UINT32_MAX);
     uint64_t begin = 0, rows_at = 0;
     for (int32_t i = 0; i < a.count; ++i) {
       const skv_attn_request& q = *some.r[i];
@@ -352,14 +359,15 @@ skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* r
       r.v = static_cast<const uint16_t*>(q.v);
       r.out = static_cast<uint16_t*>(q.out);
       r.lse = q.lse;
-      r.kv_token = q.kv_token_stride;
+      r.kv_token = static_cast<int32_t>(q.kv_token_stride);
       r.kv_head = q.kv_head_stride;
       r.nq = q.num_queries;
       r.nk = q.num_keys;
       r.splits = split ? p.splits[i] : 1;
-      r.begin = static_cast<uint32_t>(begin);
+      r.row_blocks = static_cast<int32_t>(prompt_blocks(cfg, q, 32 * a.row_tiles) / a.H);
       r.rows_at = static_cast<uint32_t>(rows_at);
-      begin += static_cast<uint64_t>(prompt_blocks(cfg, q, 32 * a.row_tiles)) * static_cast<uint64_t>(r.splits);
+      a.begin[i] = static_cast<uint32_t>(begin);
+      begin += static_cast<uint64_t>(r.row_blocks) * static_cast<uint64_t>(a.H) * static_cast<uint64_t>(r.splits);
       if (r.splits > 1) rows_at += static_cast<uint64_t>(q.num_queries) * cfg->num_q_heads * r.splits;
     }
     a.blocks = static_cast<uint32_t>(begin);
@@ -442,6 +450,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   a.tail_parts = p.tail_parts;
   a.tail_blocks = p.tail_blocks;
   a.tail_tiles = p.tail_tiles;
+  a.tail_least = p.tail_least;
   a.prefix_groups = static_cast<uint32_t>(p.prefix_groups);
   a.groups = static_cast<uint32_t>(p.groups);
   a.alpha = c.scale * kLog2e;

@@ -18,10 +18,11 @@ struct PromptDesc {
   const uint16_t* v;
   uint16_t* out;
   float* lse;  // [num_queries][Hq], may be null
-  int64_t kv_token, kv_head;
+  int64_t kv_head;
+  int32_t kv_token;
   int32_t nq, nk;
   int32_t splits;    // parts of the key range, joined by a second launch where > 1
-  uint32_t begin;    // the request's first workgroup
+  int32_t row_blocks;
   uint32_t rows_at;  // splits > 1: the request's first row in the partial results
 };
 
@@ -34,6 +35,8 @@ struct PromptArgs {
   int64_t q_token, q_head, out_token, out_head;
   float* part_o;        // partial results: binary32 [rows][d], unnormalized
   float* part_ml;       // [rows][2]: reference and sum
+  Divider by_H, by_G;
+  uint32_t begin[kMaxPromptBatch];  // the requests' first workgroups; past the last, 2^32 - 1
   PromptDesc r[kMaxPromptBatch];
 };
 static_assert(sizeof(PromptArgs) <= 4000, "kernel arguments");
@@ -67,7 +70,7 @@ struct DecodeArgs {
   int64_t tail_at;       // first tail row of the partial results
   int32_t B, Lq, H, G, num_blocks, block_size, width, prefix, tier_len;
   int32_t prefix_parts, prefix_blocks, prefix_tiles, prefix_chunk;  // row blocks, 32-row tiles of one, tokens of a part
-  int32_t tail_parts, tail_blocks, tail_tiles;
+  int32_t tail_parts, tail_blocks, tail_tiles, tail_least;  // the last: 64-token tiles of a part, at least
   int32_t direct;                  // no parts: results are written at once
   uint32_t prefix_groups, groups;  // workgroups of the prefix, of the launch
   float alpha;
