@@ -215,6 +215,8 @@ struct WaveAttention {
       for (int u = 0; u < 2; ++u) vaddr[dt][u] += bytes;
   }
 
+  // Whether this wave multiplies (the others load tiles only).
+  __device__ __forceinline__ bool multiplies() const { return ks < streams; }
   __device__ __forceinline__ void load_q(const void* row) {
     const uint8_t* p = static_cast<const uint8_t*>(row) + 16 * ((threadIdx.x >> 5) & 1);
 #pragma unroll

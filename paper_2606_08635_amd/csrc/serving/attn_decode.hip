@@ -109,7 +109,9 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
   const uint32_t token = a.by_G.div(row), g = row - token * a.G;
   const uint32_t b = a.by_Lq.div(token), i = token - b * a.Lq;
   const int head = h * a.G + static_cast<int>(g);
-  w.load_q(a.q + b * a.q_request + i * a.q_token + head * a.q_head);
+  // (with one row tile most waves only load: without their queries 16 x 256, one
+  // request of 1000 tokens: 13.3 -> 12.8 us)
+  if (w.multiplies()) w.load_q(a.q + b * a.q_request + i * a.q_token + head * a.q_head);
   const int len = min(max(a.lens[b], 0), a.width * a.block_size);
   const int limit = len - a.Lq + static_cast<int>(i);  // the row's last visible position
   int wave_min = limit;
