@@ -11,6 +11,12 @@
  * compacted payload (Algorithm 1, transfer).  On the decode side it dequantizes
  * the payload into an fp16 paged KV cache (Sec. 4.2, Fig. "sysarch").
  *
+ * Beside the codec stand the operators that its callers run next to it (at the end
+ * of this file): attention over the prompts whose K and V it packs
+ * (skv_attn_prompt), attention of new tokens over the paged cache with dropped
+ * tokens masked and a shared prefix read once (skv_attn_decode), and the pages of
+ * that cache (skv_pages_*: reserve, fork, compact, free, copy).
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - Pointers named k, v, q_obs, score, tier, payload, k_cache, v_cache,

@@ -3,8 +3,9 @@
 Argument marshalling only: every function checks that the torch tensors it is
 given have the dtype, device and size the configuration implies (the C library
 cannot see device buffer sizes), passes their ``data_ptr()`` and the current
-HIP stream, and raises ``SkvError`` on a nonzero status.  All codec work runs
-in the library's HIP kernels; there is no fallback.  If ``libskv.so`` has not
+HIP stream, and raises ``SkvError`` on a nonzero status.  All work, the codec's and
+that of the attention and page operators (``attn_*``, ``pages_*``), runs in the
+library's HIP kernels; there is no fallback.  If ``libskv.so`` has not
 been built, the first call raises.
 """
 import ctypes
