@@ -608,7 +608,8 @@ skv_status skv_attn_prompt_workspace_size(const skv_attn_config* cfg, const skv_
  * skv_attn_prompt_workspace_size bytes, sequences with few queries and many keys
  * run split over the GPU (results differ from the unsplit ones by rounding
  * alone), with less they run unsplit.  Calls that share ws must be ordered on one
- * stream.  Every request is checked before anything is enqueued.  Kernel
+ * stream.  Every request is checked before anything is enqueued (SKV_ERR_CAPACITY:
+ * more than 2^21 workgroups of up to 128 rows and a KV head in a launch).  Kernel
  * launches only: the call can be captured in a HIP graph. */
 skv_status skv_attn_prompt(const skv_attn_config* cfg, const skv_attn_request* reqs, int32_t count, void* ws,
                            uint64_t ws_bytes, hipStream_t stream);
@@ -658,8 +659,9 @@ skv_status skv_attn_decode_workspace_size(const skv_decode_config* cfg, uint64_t
  * SKV_ERR_FORMAT where a table entry in use is outside [0, num_blocks) (its
  * tokens are left out) or a length outside [0, table_width * block_size] (taken to
  * the nearer end); never cleared, so one check serves many steps.  ws:
- * skv_attn_decode_workspace_size bytes (ws_bytes; SKV_ERR_CAPACITY if less), may
- * be NULL where that is 0.  Calls that share ws must be ordered on one stream.
+ * skv_attn_decode_workspace_size bytes (ws_bytes; SKV_ERR_CAPACITY if less, or for
+ * more than 2^21 workgroups: B H, per 128 of a request's Lq Hq / H rows), may be
+ * NULL where that is 0.  Calls that share ws must be ordered on one stream.
  * Alignment 16 (tables, lens, lse, dev_status 4, tiers any).  Kernel launches
  * only: the call can be captured in a HIP graph. */
 skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const void* k_cache, const void* v_cache,

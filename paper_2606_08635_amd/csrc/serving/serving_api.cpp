@@ -400,7 +400,7 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
   if (tiers != nullptr && (c.tier_len < 0 || c.tier_request_stride < 0 || c.tier_head_stride < 0)) return SKV_ERR_INVALID_ARG;
   if (c.num_requests == 0 || c.num_queries == 0) return SKV_OK;
   if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(lens, 4) ||
-      !aligned(tables, 4) || (lse != nullptr && !aligned(lse, 4)) || (dev_status != nullptr && !aligned(dev_status, 4)))
+      (c.table_width > 0 && !aligned(tables, 4)) || (lse != nullptr && !aligned(lse, 4)) || (dev_status != nullptr && !aligned(dev_status, 4)))
     return SKV_ERR_INVALID_ARG;
   const DecodePlan p = plan_decode(cfg);
   if (p.bytes > 0 && !aligned(ws, 16)) return SKV_ERR_INVALID_ARG;

@@ -735,6 +735,8 @@ def _pool(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: Optional[torch.Ten
     if dtype not in _ATTN_TYPES:
         raise TypeError(f"caches must be float16 or bfloat16, got {dtype}")
     L, nb, bs, H, d = shape
+    if refs is not None and refs.numel() != nb:
+        raise ValueError(f"refs must hold one count per page, {nb}, got {refs.numel()}")
     return _PAGE_POOL.pack(L, nb, bs, 2 * H * d, _flat(k_cache, dtype, device, 0, "k_cache"),
                            _flat(v_cache, dtype, device, 0, "v_cache"),
                            0 if refs is None else _flat(refs, torch.int32, device, nb, "refs"))
@@ -774,7 +776,8 @@ def pages_fork(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tensor,
                lens: torch.Tensor, parents: torch.Tensor, out_tables: torch.Tensor, out_lens: torch.Tensor,
                ws: torch.Tensor, dev_status: torch.Tensor, stream=None):
     """Child c becomes a copy of request parents[c]: full pages shared, a partly
-    filled last page copied.  Writes out_tables [children][width] and out_lens."""
+    filled last page copied.  Writes out_tables [children][width] and out_lens,
+    which may not be the inputs."""
     B, N, device = lens.numel(), parents.numel(), refs.get_device()
     pool = _pool(k_cache, v_cache, refs, device)
     tp, width = _tables(tables, B, device, "tables")
@@ -793,7 +796,7 @@ def pages_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, refs: torch.Tens
     """Copies of the requests without their DROP tokens (tiers: uint8
     [B][tier_len], any request stride; tokens past tier_len are kept): full
     pages before the first dropped token shared, the other rows gathered into
-    new pages."""
+    new pages.  out_tables and out_lens may not be the inputs."""
     B, device = lens.numel(), refs.get_device()
     pool = _pool(k_cache, v_cache, refs, device)
     tp, width = _tables(tables, B, device, "tables")

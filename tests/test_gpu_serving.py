@@ -222,3 +222,25 @@ def test_arguments_refused():
         a.update(change)
         with pytest.raises((ValueError, TypeError, skv.SkvError)):
             skv.attn_decode(qd, a["k"], a["v"], a["tables"], a["lens"], a["out"], None, 20, **kw)
+
+
+def test_tables_of_no_width():
+    """Requests without pages see nothing."""
+    cache, q = torch.zeros(5, 16, 2, 64, dtype=torch.float16, device=DEV), torch.randn(3, 1, 4, 64, device=DEV).half()
+    tables, lens = torch.zeros(3, 0, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    out, lse, bad = torch.ones_like(q), torch.zeros(3, 1, 4, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    skv.attn_decode(q, cache, cache, tables, lens, out, None, 0, lse=lse, dev_status=bad)
+    assert (out == 0).all() and (lse == -float("inf")).all() and bad.item() == 0
+
+
+def test_pools_of_another_size_refused():
+    cache = torch.zeros(1, 8, 16, 2, 64, dtype=torch.float16, device=DEV)
+    tables, one = torch.zeros(1, 2, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(skv.pages_workspace_size(1, 9, 32), dtype=torch.uint8, device=DEV)
+    for pages in (7, 9):
+        refs = torch.zeros(pages, dtype=torch.int32, device=DEV)
+        with pytest.raises(ValueError):
+            skv.pages_fork(cache, cache, refs, tables, one, one, tables.clone(), one.clone(), ws, one.clone())
+    refs = torch.zeros(8, dtype=torch.int32, device=DEV)
+    with pytest.raises(skv.SkvError):  # in place
+        skv.pages_fork(cache, cache, refs, tables, one, one.clone(), tables, one, ws, one.clone())

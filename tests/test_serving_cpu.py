@@ -199,6 +199,7 @@ def test_sizes_past_the_limits_refused(lib):
     """Just past what a launch and the kernels' indexes hold: refused by the host."""
     assert _decode(lib, B=1 << 10, Lq=1 << 10, Hq=64, H=64) == BAD
     assert _decode(lib, width=(1 << 26) + 1, ts=(1 << 26) + 1) == BAD
+    assert _decode(lib, B=1 << 19, Hq=8, H=8, max_len=10) == skv.ERR_CAPACITY
     # 48 small requests and one that no grid holds: nothing of it is launched
     cfg = skv._ATTN_CONFIG.pack(0, 4096, 4096, 32, 1, 0.1, 1 << 17, 32, 1 << 17, 32)
     small, huge = (skv._ATTN_REQUEST.pack(n, n, P, P, P, P, 0, 1 << 17, 32) for n in (1, 1 << 20))
