@@ -673,6 +673,21 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// op over the wave's 64 lanes (all active), in every lane; op is commutative.
+template <class Op>
+__device__ __forceinline__ float over_wave(float v, Op op) {
+  auto moved = [](uint32_t x) { return __builtin_bit_cast(float, x); };
+  auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
+  const LanePair a = lane_pair16(bits(v));
+  v = op(moved(a.lo), moved(a.hi));
+  v = op(v, moved(dpp_mov<0x140>(bits(v))));  // lanes i and 15 - i
+  v = op(v, moved(dpp_mov<0x141>(bits(v))));  // i and 7 - i
+  v = op(v, moved(dpp_mov<0xB1>(bits(v))));   // i and i ^ 1
+  v = op(v, moved(dpp_mov<0x4E>(bits(v))));   // i and i ^ 2
+  const LanePair b = lane_pair32(bits(v));
+  return op(moved(b.lo), moved(b.hi));
+}
+
 // Joins the parts of a row.  WAVES waves of a workgroup share it, every WAVES-th
 // part to each; a lane has D / 64 channels (at D = 32 the upper half of a wave
 // repeats the lower).  A wave reads the references and sums of 64 parts at once, and
@@ -699,14 +714,10 @@ struct JoinedRow {
       vec x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const vec*>(po + (from + min(i, n - 1) * WAVES * stride) * D);
-      float top = ml.x;
-#pragma unroll
-      for (int y = 32; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
+      const float top = over_wave(ml.x, [](float a, float b) { return fmaxf(a, b); });
       const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
       const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
-      float sum = ml.y * f;  // 0 of a part that saw nothing
-#pragma unroll
-      for (int y = 32; y > 0; y >>= 1) sum += __shfl_xor(sum, y);
+      const float sum = over_wave(ml.y * f, [](float a, float b) { return a + b; });  // 0 of a part that saw nothing
       l = l * keep + sum;
       m = mn;
 #pragma unroll
@@ -722,7 +733,7 @@ struct JoinedRow {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if (s + i >= n) break;
-          const float fs = __shfl(f, s + i);
+          const float fs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s + i));
           const bool use = seen >> (s + i) & 1;
 #pragma unroll
           for (int c = 0; c < kPer; ++c) o[c] += (use ? x[i][c] : 0.0f) * fs;
@@ -765,7 +776,9 @@ struct JoinedRow {
       if (D >= 64 || lane < D) out[kPer * lane + i] = static_cast<typename E::elem>(o[i] * inv);
   }
 };
-// Rows for which a wave each would leave most of the GPU idle get four.
-constexpr uint64_t kFewRows = 2048;
+// Rows for which a wave each would leave most of the GPU idle get four (2048 rows of 17
+// parts, with the launch before: 39 us by four waves, 37 by one; 1024 rows of 33: 25.0
+// and 26.2).
+constexpr uint64_t kFewRows = 1024;
 
 }  // namespace skv
