@@ -214,3 +214,21 @@ def test_graph_follows_lengths_and_tables():
         # bit for bit: the last replay's first request reads rows that hold NaN
         assert torch.equal(out.view(torch.int16), want.view(torch.int16))
         assert torch.equal(lse.view(torch.int32), want_lse.view(torch.int32))
+
+
+@pytest.mark.parametrize("d,Hq,H", [(32, 4, 4), (128, 32, 8), (256, 8, 4)])
+@pytest.mark.parametrize("count", [31, 35])
+def test_joins_of_few_and_many_rows(count, Hq, H, d):
+    """Rows joined by four waves and by one, parts of the prefix and of uneven tails; more requests than a wave's lanes
+    hold at once are cut whole (test_more_requests_than_are_cut)."""
+    lens = [640 + (900 * i) % 3001 for i in range(count)]
+    b = Batch(lens, Hq, H, d, prefix=640, tier_len=2000, drop=0.6, seed=count)
+    check(*b.run(), b.want(), (count, d))
+
+
+def test_more_requests_than_are_cut():
+    """257 requests: none is cut, the prefix still is; a long one among short ones."""
+    lens = [256 + i % 3 for i in range(257)]
+    lens[100], lens[256] = 1500, 0
+    b = Batch(lens, 4, 4, 64, prefix=256, seed=9)
+    check(*b.run(), b.want())
