@@ -147,10 +147,10 @@ DecodePlan plan_decode(const skv_decode_config* c) {
   // The prefix gets the share of the room that its tiles are of all (one of many rows
   // counted twice, the tails taken to be half as long as the longest), at most half:
   // more parts are more partial results to write and join (64 requests behind 16384
-  // tokens of 8 x 128: 47 us with 512 workgroups, 40 with 256, 47 with 128).  By its
-  // share against always half: 64 behind 2048 with up to 3800 of their own, 123 us
-  // against 139; 12 behind 2048 of 8 x 256, 5 queries each, with up to 1450, 34
-  // against 47.
+  // tokens of 8 x 128, 0.4 of them dropped: 45 us with all of the room at most, 38 with
+  // half, 47 with a quarter).  By its share against always half: 64 behind 2048 with
+  // up to 3800 of their own, 123 us against 139; 12 behind 2048 of 8 x 256, 5 queries
+  // each, with up to 1450, 34 against 47.
   if (c->prefix_len > 0) {
     p.prefix_tiles = row_tiles(all);
     p.prefix_blocks = static_cast<int32_t>(up(all, 32 * p.prefix_tiles));
