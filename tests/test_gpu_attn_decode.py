@@ -219,8 +219,7 @@ def test_graph_follows_lengths_and_tables():
 @pytest.mark.parametrize("d,Hq,H", [(32, 4, 4), (128, 32, 8), (256, 8, 4)])
 @pytest.mark.parametrize("count", [31, 35])
 def test_joins_of_few_and_many_rows(count, Hq, H, d):
-    """Rows joined by four waves and by one, parts of the prefix and of uneven tails; more requests than a wave's lanes
-    hold at once are cut whole (test_more_requests_than_are_cut)."""
+    """Rows joined by four waves and by one, parts of the prefix and of uneven tails."""
     lens = [640 + (900 * i) % 3001 for i in range(count)]
     b = Batch(lens, Hq, H, d, prefix=640, tier_len=2000, drop=0.6, seed=count)
     check(*b.run(), b.want(), (count, d))

@@ -244,3 +244,51 @@ def test_pools_of_another_size_refused():
     refs = torch.zeros(8, dtype=torch.int32, device=DEV)
     with pytest.raises(skv.SkvError):  # in place
         skv.pages_fork(cache, cache, refs, tables, one, one.clone(), tables, one, ws, one.clone())
+
+
+def test_graphs_on_one_workspace_and_two_streams():
+    """Two captured calls share a workspace and are replayed in turn; two streams run calls of their own at once."""
+    Hq, H, d, block = 8, 2, 128, 16
+    g = torch.Generator(device=DEV).manual_seed(11)
+    new = lambda *shape: torch.randn(*shape, generator=g, device=DEV).half()
+    kc, vc = new(500, block, H, d), new(500, block, H, d)
+    tables = torch.randperm(500, generator=g, device=DEV)[:480].int().view(4, 120)
+    lens = torch.tensor([1900, 700, 1, 1200], dtype=torch.int32, device=DEV)
+    q1, q2, kp, vp = new(4, 1, Hq, d), new(50, Hq, d), new(3000, H, d), new(3000, H, d)
+    size = max(skv.attn_decode_workspace_size(4, 1, Hq, H, d, 1900), skv.attn_prompt_workspace_size([50], [3000], Hq, H, d))
+    assert min(skv.attn_decode_workspace_size(4, 1, Hq, H, d, 1900), skv.attn_prompt_workspace_size([50], [3000], Hq, H, d)) > 0
+
+    def decode(out, ws):
+        skv.attn_decode(q1, kc, vc, tables, lens, out, ws, 1900)
+
+    def prompt(out, ws):
+        skv.attn_prompt(q2, kp, vp, out, [50], [3000], ws=ws)
+
+    room = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    want = [torch.empty_like(q1), torch.empty_like(q2)]
+    decode(want[0], room[0])
+    prompt(want[1], room[0])
+    outs = [torch.empty_like(q1), torch.empty_like(q2)]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph, call, out in zip(graphs, (decode, prompt), outs):
+        with torch.cuda.graph(graph):
+            call(out, room[1])
+    for turn in range(4):
+        for out in outs:
+            out.fill_(5.0)
+        room[1].fill_(0xFF)
+        for i in (turn % 2, 1 - turn % 2):
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(outs, want))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    results = [[], []]
+    for turn in range(8):
+        for i, (s, call) in enumerate(zip(streams, (decode, prompt))):
+            with torch.cuda.stream(s):
+                out = torch.empty_like(want[i])
+                call(out, room[1 + i])
+                results[i].append(out)
+    torch.cuda.synchronize()
+    for got, w in zip(results, want):
+        assert all(torch.equal(x.view(torch.int16), w.view(torch.int16)) for x in got)
