@@ -173,9 +173,13 @@ __device__ __forceinline__ void lds_barrier() {
 // lds_base + 16 * lane.  Issued from inline assembly so that the
 // compiler does not count it among its own loads: the stage loop waits for it
 // explicitly (wait_stage), and the compiler's own waits for its loads stay
-// correct because they can only wait longer.
+// correct because they can only wait longer.  A load that reads m0 needs one wait
+// state behind the write of it, which the compiler does not add inside the
+// statement: the s_nop.  (m0 on the clobber list tells the compiler that its own
+// value is gone; it warns that it would not save one, and it keeps none there
+// across statements.)
 __device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(src), "s"(lds_base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(src), "s"(lds_base) : "memory", "m0");
 }
 
 // Issues the direct loads of keys t0 .. t0 + kKeys - 1 into the stage at sk.

@@ -224,13 +224,14 @@ __global__ __launch_bounds__(kThreads) void stage_direct(const uint8_t* __restri
 #pragma unroll
     for (int u = 0; u < kStagePieces; ++u) {
       // the wave's 64 lanes land 16 bytes each at consecutive LDS addresses from m0
+      // (a load that reads m0 needs one wait state behind the write of it: the s_nop)
       const uint32_t m0 = lds + (st % NB) * kStageBytes + (u * kThreads + wave * 64) * 16;
       const uint8_t* p = blk + st * kStageBytes + (u * kThreads + threadIdx.x) * 16;
       if (NT)
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(p), "s"(__builtin_amdgcn_readfirstlane(m0))
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(p), "s"(__builtin_amdgcn_readfirstlane(m0))
                      : "memory", "m0");
       else
-        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(__builtin_amdgcn_readfirstlane(m0))
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(__builtin_amdgcn_readfirstlane(m0))
                      : "memory", "m0");
     }
   };

@@ -74,7 +74,9 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // Direct global-to-LDS load: lane i's 16 bytes at src land at LDS byte address
 // lds_base + 16 i.  From inline assembly, so that the compiler does not count it
 // among its own loads; the tile loop waits for it itself (wait_direct_loads).  A
-// load that reads m0 needs one wait state behind the write of it: the s_nop.
+// load that reads m0 needs one wait state behind the write of it: the s_nop.  (m0 on
+// the clobber list tells the compiler that its own value is gone; it warns that it
+// would not save one, and it keeps none there across statements.)
 __device__ __forceinline__ void direct_load(const void* src, uint32_t lds_base) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds_base) : "memory", "m0");
 }
