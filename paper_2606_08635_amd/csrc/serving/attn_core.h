@@ -42,6 +42,7 @@ struct TypeF16 {
   typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
   typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
   static constexpr uint16_t kInf = 0x7C00, kOne = 0x3C00;
+  static constexpr float kTop = 8.0f;  // log2 of a row's largest probability when its reference is set
   __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -51,6 +52,7 @@ struct TypeBF16 {
   typedef __bf16 vec8 __attribute__((ext_vector_type(8)));
   typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
   static constexpr uint16_t kInf = 0x7F80, kOne = 0x3F80;
+  static constexpr float kTop = 0.0f;
   __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -163,8 +165,13 @@ struct WaveAttention {
   // A step is exponentiated against the current reference m first, without its
   // maximum; only where that gives a sum past kHigh (or a NaN: m still -inf) is
   // the maximum taken, m raised and o rescaled.  2^15 keeps every probability
-  // inside binary16.  m is some earlier step's maximum, so what underflows
-  // against it is negligible beside what is in the sum already.
+  // inside binary16.  m is some earlier step's maximum less E::kTop, so the largest
+  // probability of the sum so far is at least 2^kTop.  What rounds to 0 for the second
+  // product is added to l all the same, so many such keys would be missing from o
+  // alone: binary16 ends at 2^-25, and with kTop = 8 that is 2^-33 of the largest
+  // (2^20 keys just below it are 2^-13 of the result, under half a step of its type),
+  // with room for 32 keys at the maximum and for references 2^2 to 2^7 too low.
+  // bfloat16 ends far below either way and leaves the room to V.
   static constexpr float kHigh = 32768.0f;
   static constexpr uint16_t kInf = E::kInf, kOne1 = E::kOne;
   static constexpr int kAhead = 4;  // operands read ahead of their products
@@ -298,7 +305,7 @@ struct WaveAttention {
     }
     return sum;
   }
-  // The row's largest logit, times alpha (both lane-halves get it).
+  // The reference that puts the row's largest logit at 2^kTop (both lane-halves get it).
   template <int N>
   __device__ __forceinline__ float largest(const floatx16 (&x)[N], float alpha) const {
     float top = -INFINITY;
@@ -307,7 +314,7 @@ struct WaveAttention {
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, x[n][r]);
     const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, top * alpha));
-    return fmaxf(__builtin_bit_cast(float, p.lo), __builtin_bit_cast(float, p.hi));
+    return fmaxf(__builtin_bit_cast(float, p.lo), __builtin_bit_cast(float, p.hi)) - E::kTop;
   }
   // Whether no row has a reference yet: the first step takes the maximum at once.
   __device__ __forceinline__ bool fresh() const { return __all(m == -INFINITY); }
