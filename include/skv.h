@@ -561,9 +561,9 @@ skv_status skv_link(void* dst, const void* src, uint64_t bytes, void* host_stagi
  * -infinity.  Query head hq reads KV head hq / (Hq / H).  Products are exact,
  * sums binary32, probabilities rounded to the 16-bit type before their product
  * with V, results rounded once.  NaN and infinities follow IEEE softmax over the
- * visible keys (but a key whose probability underflows to 0 has no effect, where
+ * visible keys (but a key whose probability underflows to 0 may have no effect, where
  * IEEE's 0 times infinity is NaN: in binary16 one below 2^-33 of the row's largest);
- * hidden keys' K and V, whatever they hold, have no effect.
+ * finite V give finite results; hidden keys' K and V, whatever they hold, have no effect.
  * Results of a call are the same every time. */
 enum { SKV_DTYPE_F16 = 0, SKV_DTYPE_BF16 = 1 };
 

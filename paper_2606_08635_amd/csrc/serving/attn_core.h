@@ -37,12 +37,15 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
+constexpr float kRoom = 16.0f;  // log2 of the parts of a row whose sums are added without overflow
+
 struct TypeF16 {
   typedef _Float16 elem;
   typedef _Float16 vec8 __attribute__((ext_vector_type(8)));
   typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
   static constexpr uint16_t kInf = 0x7C00, kOne = 0x3C00;
   static constexpr float kTop = 8.0f;  // log2 of a row's largest probability when its reference is set
+  static constexpr bool kWide = false;  // whether sums of V times unnormalized probabilities can pass binary32
   __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -53,6 +56,7 @@ struct TypeBF16 {
   typedef __bf16 vec2 __attribute__((ext_vector_type(2)));
   static constexpr uint16_t kInf = 0x7F80, kOne = 0x3F80;
   static constexpr float kTop = 0.0f;
+  static constexpr bool kWide = true;
   __device__ static __forceinline__ floatx16 mfma(vec8 a, vec8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -353,6 +357,27 @@ struct WaveAttention {
     m = -INFINITY;
     l = 0.0f;
   }
+  // Before a second walk.  Where V's type reaches as far as binary32, a sum of
+  // unnormalized probabilities times V can overflow although the average is finite;
+  // the first walk's m and l are the row's log-sum, and against 2^kRoom times that the
+  // probabilities add up to 2^-kRoom: no sum of theirs, and none of up to 2^kRoom
+  // parts', passes V's largest.
+  __device__ __forceinline__ void again(AreaType& area) {
+    float ref = -INFINITY;
+    if constexpr (E::kWide) {
+      const LanePair p = lane_pair32(__builtin_bit_cast(uint32_t, l));
+      float sum = __builtin_bit_cast(float, p.lo) + __builtin_bit_cast(float, p.hi);
+      if constexpr (F == kPair) {
+        const int lane = threadIdx.x & 31;
+        if (ks < 2) area.l[rt][ks][lane] = sum;
+        stage_barrier();
+        if (ks < 2) sum = area.l[rt][0][lane] + area.l[rt][1][lane];
+      }
+      ref = m + __builtin_amdgcn_logf(sum) + kRoom;
+    }
+    reset();
+    if (__builtin_fabsf(ref) < INFINITY) m = ref;
+  }
   // Whether the sums hold an infinity or NaN.
   __device__ __forceinline__ bool not_finite() const {
     float t = 0.0f;
@@ -578,7 +603,7 @@ struct WaveAttention {
   __device__ __forceinline__ void merge_state(const uint8_t* from) {
     const floatx4* f = reinterpret_cast<const floatx4*>(from) + (threadIdx.x & 63);
     const floatx2 ml = reinterpret_cast<const floatx2*>(f - (threadIdx.x & 63) + 64 * 4 * kTiles)[threadIdx.x & 63];
-    const float mn = fmaxf(m, ml.x), ref = mn == -INFINITY ? 0.0f : mn;
+    const float mn = fmaxf(m, ml.x) + 1.0f, ref = mn == -INFINITY ? 0.0f : mn;  // (halves of two finite sums add up to one)
     const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(ml.x - ref);
     m = mn;
     l = l * a + ml.y * b;
@@ -662,7 +687,8 @@ __device__ __forceinline__ void walk_once(Wave& w, int t0, int t1, Issue issue, 
 // the first time let an infinity or NaN of V reach rows from which it is hidden (0
 // times it is NaN), and second terms make NaN of one that is seen; so where a result
 // is not finite, everything is done again by accumulate_safe, whose arithmetic would
-// cost the first loop its registers.  Ends with a barrier: the stage is free.
+// cost the first loop its registers, and against a reference that lets no sum overflow
+// (again).  Ends with a barrier: the stage is free.
 template <class Wave, class AreaType, class Walk>
 __device__ __forceinline__ void walk_tiles(Wave& w, AreaType& area, Walk walk) {
   if (threadIdx.x == 0) area.not_finite = 0;
@@ -671,7 +697,7 @@ __device__ __forceinline__ void walk_tiles(Wave& w, AreaType& area, Walk walk) {
   if (w.not_finite()) area.not_finite = 1;
   stage_barrier();
   if (__builtin_expect(*const_cast<volatile int32_t*>(&area.not_finite) != 0, 0)) {
-    w.reset();
+    w.again(area);
     walk(std::integral_constant<bool, true>{});
     stage_barrier();
   }
@@ -699,7 +725,8 @@ __device__ __forceinline__ float over_wave(float v, Op op) {
 
 // Joins the parts of a row.  WAVES waves of a workgroup share it, every WAVES-th
 // part to each; a lane has D / 64 channels (at D = 32 the upper half of a wave
-// repeats the lower).  A wave reads the references and sums of 64 parts at once, and
+// repeats the lower).  Finite parts are added against a reference 2^kRoom times their
+// largest, so that their sum is finite too.  A wave reads the references and sums of 64 parts at once, and
 // eight parts' sums are in flight together.
 template <int D, int WAVES>
 struct JoinedRow {
@@ -724,7 +751,7 @@ struct JoinedRow {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const vec*>(po + (from + min(i, n - 1) * WAVES * stride) * D);
       const float top = over_wave(ml.x, [](float a, float b) { return fmaxf(a, b); });
-      const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.0f : mn;
+      const float mn = fmaxf(m, top + kRoom), ref = mn == -INFINITY ? 0.0f : mn;
       const float keep = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
       const float sum = over_wave(ml.y * f, [](float a, float b) { return a + b; });  // 0 of a part that saw nothing
       l = l * keep + sum;
