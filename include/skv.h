@@ -557,13 +557,14 @@ skv_status skv_link(void* dst, const void* src, uint64_t bytes, void* host_stagi
 /* Attention beside the codec: over the prompts whose K and V it packs, and over
  * the paged cache it fills.  For a query with visible keys t the result is
  * out = sum_t softmax_t(scale q.k_t) v_t and lse = log sum_t exp(scale q.k_t)
- * (natural logarithm); a query that sees no key gets out = 0 and lse =
- * -infinity.  Query head hq reads KV head hq / (Hq / H).  Products are exact,
- * sums binary32, probabilities rounded to the 16-bit type before their product
- * with V, results rounded once.  NaN and infinities follow IEEE softmax over the
- * visible keys (but a key whose probability underflows to 0 may have no effect, where
- * IEEE's 0 times infinity is NaN: in binary16 one below 2^-33 of the row's largest);
- * finite V give finite results; hidden keys' K and V, whatever they hold, have no effect.
+ * (natural logarithm); a query that sees no key gets out = 0 and lse = -infinity (one
+ * that sees keys whose logits are all -infinity gets out = NaN).  Query head hq reads
+ * KV head hq / (Hq / H).  Products are exact, sums binary32, probabilities rounded to
+ * the 16-bit type before their product with V, results rounded once.  NaN and
+ * infinities follow IEEE softmax over the visible keys (but a key whose probability
+ * underflows to 0 may have no effect, where IEEE's 0 times infinity is NaN: in binary16
+ * one below 2^-33 of the row's largest); finite V give finite results; hidden keys' K
+ * and V, whatever they hold, have no effect.
  * Results of a call are the same every time. */
 enum { SKV_DTYPE_F16 = 0, SKV_DTYPE_BF16 = 1 };
 

@@ -703,7 +703,15 @@ __device__ __forceinline__ void walk_tiles(Wave& w, AreaType& area, Walk walk) {
   }
 }
 
-__device__ __forceinline__ float inverse_or_zero(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+// A row's sum l is 0 where it sees no key (its result is 0), and where the logits of
+// all the keys it sees are -infinity: softmax over those is NaN (exp(-inf - -inf)).
+// `saw`: whether it sees a key.
+__device__ __forceinline__ float inverse_sum(float l, bool saw) {
+  return l == 0.0f ? (saw ? NAN : 0.0f) : 1.0f / l;
+}
+// l of a part as it is written beside m: 1 with m = -infinity where the part's logits
+// are all -infinity, which weighs nothing beside another part.
+__device__ __forceinline__ float part_sum(float l, bool saw) { return l == 0.0f && saw ? 1.0f : l; }
 __device__ __forceinline__ float log_sum(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
@@ -734,8 +742,10 @@ struct JoinedRow {
   typedef float vec __attribute__((ext_vector_type(kPer)));
   struct Shared {
     float m[4], l[4], o[4][64 * kPer];
+    int32_t saw[4];
   };
   float m = -INFINITY, l = 0.0f, o[kPer] = {};
+  bool saw = false;  // a part's keys, with logits of -infinity all of them (part_sum)
 
   // Part s is row first + s * stride of the partial results.
   __device__ __forceinline__ void add(const float* part_o, const float* part_ml, int64_t first, int64_t stride, int parts) {
@@ -759,6 +769,7 @@ struct JoinedRow {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) o[i] *= keep;
       const uint64_t seen = __ballot(ml.x != -INFINITY || ml.y != 0.0f);  // the others may have written no sums
+      saw |= __any(ml.x == -INFINITY && ml.y > 0.0f);
       for (int s = 0; s < n; s += 8) {
         vec next[8];
         if (s + 8 < n) {
@@ -786,6 +797,7 @@ struct JoinedRow {
       if (lane == 0) {
         sh.m[wave] = m;
         sh.l[wave] = l;
+        sh.saw[wave] = saw;
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) sh.o[wave][kPer * lane + i] = o[i];
@@ -796,6 +808,7 @@ struct JoinedRow {
         const float mn = fmaxf(m, sh.m[w]), ref = mn == -INFINITY ? 0.0f : mn;
         const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(sh.m[w] - ref);
         m = mn;
+        saw |= sh.saw[w] != 0;
         l = l * a + sh.l[w] * b;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) o[i] = o[i] * a + sh.o[w][kPer * lane + i] * b;
@@ -806,7 +819,7 @@ struct JoinedRow {
   template <class E>
   __device__ __forceinline__ void write(typename E::elem* out) const {
     const int lane = threadIdx.x & 63;
-    const float inv = inverse_or_zero(l);
+    const float inv = inverse_sum(l, saw);
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
       if (D >= 64 || lane < D) out[kPer * lane + i] = static_cast<typename E::elem>(o[i] * inv);

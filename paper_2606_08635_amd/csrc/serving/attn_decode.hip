@@ -133,11 +133,13 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
   const int64_t cache_row = static_cast<int64_t>(a.H) * D;
   const uint16_t* kbase = a.k + h * D;
   const uint16_t* vbase = a.v + h * D;
+  int first_kept = INT32_MAX;  // position
   walk_tiles(w, area, [&](auto second) {
     if (decltype(second)::value) next.load(a, table, tiers, p0, min(p1, p0 + kList));
     for (int q0 = p0; q0 < p1; q0 += kList) {
       const int q1 = min(p1, q0 + kList);
       const int count = next.list(a, lists);
+      if (count > 0) first_kept = min(first_kept, lists.pos[0]);
       const int nt = (count + S::kKeys - 1) / S::kKeys;
       const bool cut = q1 - 1 > wave_min;  // some row ends before the list does
       auto issue = [&](int t, int buffer) {
@@ -168,13 +170,14 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, uint8_t* stage, type
   });
   const bool writes = w.finish(stage, area, active);
   if (!writes || mine >= rows) return;
+  const bool saw = first_kept <= limit;
   if (part_row < 0) {
-    w.write_out(a.out + b * a.out_request + i * a.out_token + head * a.out_head, inverse_or_zero(w.l));
+    w.write_out(a.out + b * a.out_request + i * a.out_token + head * a.out_head, inverse_sum(w.l, saw));
     if (a.lse != nullptr && w.writes_sum()) a.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, w.l);
     return;
   }
   w.write_partial(a.part_o + (part_row + mine) * D);
-  if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * (part_row + mine)) = floatx2{w.m, w.l};
+  if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * (part_row + mine)) = floatx2{w.m, part_sum(w.l, saw)};
 }
 
 // Tokens of request b past the prefix.

@@ -110,13 +110,14 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
   walk_tiles(w, area, [&](auto second) { walk_once<D, decltype(second)::value>(w, t0, t1, issue, tile); });
   const bool writes = w.finish(stage, area, active);
   if (!writes || row0 + (lane & 31) >= rows) return;  // (both lane-halves of a row stay: write_out pairs them)
+  const bool saw = t0 < t1 && t0 * S::kKeys <= limit;
   if (r.splits > 1) {
     const int64_t prow_at = r.rows_at + (static_cast<int64_t>(split) * a.H + h) * rows + row;
     w.write_partial(a.part_o + prow_at * D);
-    if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * prow_at) = floatx2{w.m, w.l};
+    if (w.writes_sum()) *reinterpret_cast<floatx2*>(a.part_ml + 2 * prow_at) = floatx2{w.m, part_sum(w.l, saw)};
     return;
   }
-  w.write_out(r.out + token * a.out_token + head * a.out_head, inverse_or_zero(w.l));
+  w.write_out(r.out + token * a.out_token + head * a.out_head, inverse_sum(w.l, saw));
   if (r.lse != nullptr && w.writes_sum()) r.lse[static_cast<int64_t>(token) * a.H * a.G + head] = log_sum(w.m, w.l);
 }
 
