@@ -624,7 +624,7 @@ typedef struct skv_decode_config {
                             cache (1; more to verify drafted tokens; 0: nothing
                             to do)                                                */
   int32_t num_q_heads, num_kv_heads, head_dim; /* as skv_attn_config;
-                            B Lq <= 2^20, B Lq Hq < 2^26                          */
+                            B Lq <= 2^20, B Lq Hq <= 2^26 - 4                     */
   int32_t num_blocks, block_size;              /* num_blocks * block_size < 2^31  */
   int32_t table_width;   /* entries of a request's block table; times block_size
                             at most 2^30                                          */

@@ -188,8 +188,9 @@ skv_status check_decode_sizes(const skv_decode_config* c) {
   if (c == nullptr || !shape_ok(SKV_DTYPE_F16, c->num_q_heads, c->num_kv_heads, c->head_dim, 1.0f))
     return SKV_ERR_INVALID_ARG;
   if (c->num_requests < 0 || c->num_queries < 0 || c->max_len < 0 || c->prefix_len < 0) return SKV_ERR_INVALID_ARG;
+  // (a join of 2^26 - 3 rows or more, a wave each, would be a grid of 2^32 threads, which no launch takes)
   if (static_cast<int64_t>(c->num_requests) * c->num_queries > (1 << 20) ||
-      static_cast<int64_t>(c->num_requests) * c->num_queries * c->num_q_heads >= (1 << 26))
+      static_cast<int64_t>(c->num_requests) * c->num_queries * c->num_q_heads > (1 << 26) - 4)
     return SKV_ERR_INVALID_ARG;
   return SKV_OK;
 }
