@@ -571,7 +571,7 @@ enum { SKV_DTYPE_F16 = 0, SKV_DTYPE_BF16 = 1 };
 /* What the requests of a prompt attention call share.  Strides are in elements,
  * multiples of 8, positive; a row's d elements are contiguous.  Validity: dtype
  * F16 or BF16; H >= 1, num_q_heads a multiple of H, at most 2^16; d in {32, 64,
- * 128, 256}; scale positive and finite. */
+ * 128, 256}; scale positive, and finite also times log2(e). */
 typedef struct skv_attn_config {
   int32_t dtype;        /* SKV_DTYPE_* of q, k, v and out                         */
   int32_t num_q_heads;  /* Hq                                                     */

@@ -16,7 +16,7 @@ bool aligned(const void* p, uintptr_t to) { return p != nullptr && reinterpret_c
 
 bool shape_ok(int32_t dtype, int32_t Hq, int32_t H, int32_t d, float scale) {
   return (dtype == SKV_DTYPE_F16 || dtype == SKV_DTYPE_BF16) && H >= 1 && Hq >= H && Hq <= 65536 && Hq % H == 0 &&
-         (d == 32 || d == 64 || d == 128 || d == 256) && std::isfinite(scale) && scale > 0.0f;
+         (d == 32 || d == 64 || d == 128 || d == 256) && std::isfinite(scale * kLog2e) && scale > 0.0f;
 }
 
 bool stride_ok(int64_t s) { return s > 0 && s % 8 == 0 && s < (int64_t{1} << 40); }

@@ -33,3 +33,16 @@ def test_the_largest_joins_are_not_refused():
     assert n % 1020 == 0 and _size(n // 1020, 1, 1020) == skv.OK
     assert _size(1 << 20, 1, 63) == skv.OK
     assert _size(1 << 20, 1, 64) == skv.ERR_INVALID_ARG
+
+
+def _prompt(scale):
+    cfg = skv._ATTN_CONFIG.pack(0, 4, 2, 64, 1, scale, 256, 64, 256, 64)
+    req = skv._ATTN_REQUEST.pack(0, 0, 0, 0, 0, 0, 0, 64, 64)
+    return skv.lib().skv_attn_prompt(cfg, req, 1, None, 0, None)
+
+
+@pytest.mark.parametrize("scale,status", [(2.3e38, skv.OK), (2.4e38, skv.ERR_INVALID_ARG), (3.4e38, skv.ERR_INVALID_ARG)])
+def test_scales_that_pass_binary32_in_base_2_are_refused(scale, status):
+    """The kernels multiply by scale log2(e): an infinite one would make NaN of logits of 0."""
+    assert _prompt(scale) == status
+    assert _decode(0, 1, 4, scale=scale) == status
