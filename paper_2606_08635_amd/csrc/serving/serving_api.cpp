@@ -499,8 +499,10 @@ skv_status skv_pages_fork(const skv_page_pool* pool, const int32_t* tables, int3
   a.out_tables = out_tables;
   a.out_width = out_width;
   a.out_lens = out_lens;
-  // one workgroup looks over 16384 entries in about 5 us, less than a launch more costs
-  a.checked = static_cast<int64_t>(num_children) * table_width > 16384;
+  // one workgroup looks over 2000 entries faster than a launch more costs (8 children of
+  // 4001 tokens forked, grown and released: 17.8 us against 19.5), 8000 as fast (25.1,
+  // 24.6), 16000 slower (29.4, 24.9)
+  a.checked = static_cast<int64_t>(num_children) * table_width > 8192;
   skv_status st = page_workspace(&a, 0, ws, ws_bytes);
   if (st == SKV_OK && !outputs_apart(a)) st = SKV_ERR_INVALID_ARG;
   if (st == SKV_OK) st = spread_planes(&a, std::max(1, num_children), 1024);
