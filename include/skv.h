@@ -565,6 +565,8 @@ skv_status skv_link(void* dst, const void* src, uint64_t bytes, void* host_stagi
  * underflows to 0 may have no effect, where IEEE's 0 times infinity is NaN: in binary16
  * one below 2^-33 of the row's largest); finite V give finite results; hidden keys' K
  * and V, whatever they hold, have no effect.
+ * There is no soft cap of the logits and no sliding window; layers that need one cannot
+ * be run by these calls.
  * Results of a call are the same every time. */
 enum { SKV_DTYPE_F16 = 0, SKV_DTYPE_BF16 = 1 };
 
@@ -608,7 +610,7 @@ skv_status skv_attn_prompt_workspace_size(const skv_attn_config* cfg, const skv_
  * or ws_bytes of device memory, 16-byte aligned; with at least
  * skv_attn_prompt_workspace_size bytes, sequences with few queries and many keys
  * run split over the GPU (results differ from the unsplit ones by rounding
- * alone), with less they run unsplit.  Calls that share ws must be ordered on one
+ * alone), with less they run unsplit, which can take several times as long.  Calls that share ws must be ordered on one
  * stream.  Every request is checked before anything is enqueued (SKV_ERR_CAPACITY:
  * more than 2^21 workgroups of up to 128 rows and a KV head in a launch).  Kernel
  * launches only: the call can be captured in a HIP graph. */
@@ -656,7 +658,7 @@ skv_status skv_attn_decode_workspace_size(const skv_decode_config* cfg, uint64_t
  * prefix_len are read through request 0's table and tiers, once for the batch; a
  * request that ends inside the prefix sees its own tokens of it.  lens and tables
  * are read on the device, so a captured call follows them.  out: [B][Lq][Hq][d];
- * lse: binary32 [B][Lq][Hq], or NULL.  dev_status (may be NULL): set to
+ * lse: binary32 [B][Lq][Hq], or NULL; neither may overlap the inputs.  dev_status (may be NULL): set to
  * SKV_ERR_FORMAT where a table entry in use is outside [0, num_blocks) (its
  * tokens are left out) or a length outside [0, table_width * block_size] (taken to
  * the nearer end); never cleared, so one check serves many steps.  ws:
@@ -682,14 +684,17 @@ skv_status skv_attn_decode(const skv_decode_config* cfg, const void* q, const vo
  * other than 0 a call has changed nothing else (skv_pages_free excepted, see
  * there).  ws: skv_pages_workspace_size bytes (ws_bytes; SKV_ERR_CAPACITY if less).
  * Calls on one pool, and calls that share ws or dev_status, must be ordered on one
- * stream.  At most 2^24 requests; width * block_size at most 2^30.  Alignment 16
+ * stream.  At most 2^24 requests; width * block_size at most 2^30; at most 2^21 children
+ * of a fork, and requests of a compaction times ceil(width * block_size / 256)
+ * (SKV_ERR_CAPACITY).  Alignment 16
  * (k_cache, v_cache, refs, ws), 4 (int32 arrays, dev_status).  Kernel launches
  * only: the calls can be captured in a HIP graph. */
 typedef struct skv_page_pool {
-  int32_t num_layers;  /* L                                                       */
+  int32_t num_layers;  /* L, at most 2^16                                          */
   int32_t num_blocks;  /* num_blocks * block_size < 2^31                           */
   int32_t block_size;
-  int32_t row_bytes;   /* of one token of K (or V) in a layer, 2 H d: a multiple of 16 */
+  int32_t row_bytes;   /* of one token of K (or V) in a layer, 2 H d: a multiple of 16,
+                          at most 2^24                                            */
   void* k_cache;       /* may be NULL for skv_pages_reserve and skv_pages_free     */
   void* v_cache;
   int32_t* refs;       /* not used by skv_pages_copy                               */
@@ -739,7 +744,7 @@ skv_status skv_pages_free(const skv_page_pool* pool, const int32_t* tables, int3
 /* Copies page src_pages[i] of one pool to page dst_pages[i] of another (or of the
  * same one), in every layer of K and V; the pools agree in layers, block size and
  * row bytes.  Destinations must be distinct and not among the sources of the same
- * pool. */
+ * pool.  SKV_ERR_CAPACITY for more than 2^32 pieces of 32 KB. */
 skv_status skv_pages_copy(const skv_page_pool* src, const skv_page_pool* dst, const int32_t* src_pages,
                           const int32_t* dst_pages, int32_t count, uint32_t* dev_status, hipStream_t stream);
 

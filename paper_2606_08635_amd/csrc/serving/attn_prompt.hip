@@ -13,15 +13,15 @@
 // since the last ones see the most keys and the launch ends with short ones.
 //
 // What bounds it: 4 d floating-point operations per (head, query, visible key) on the
-// matrix units.  8189 causal tokens of 32 x 128 on 8 KV heads, binary16: 513-535 us by
-// device, 1030-1070 TFLOP/s of the visible products (a large matrix product: 1140);
+// matrix units.  8189 causal tokens of 32 x 128 on 8 KV heads, binary16: 520-560 us by
+// device, 980-1060 TFLOP/s of the visible products (a large matrix product: 1140);
 // the matrix units are busy 64 % of the cycles at the clock that power then allows,
-// no bank conflicts.  8192 of 16 x 256, bfloat16: 546-568 us, 970-1010 TFLOP/s.
+// no bank conflicts.  8192 of 16 x 256, bfloat16: 550-595 us, 920-1000 TFLOP/s.
 // Staging moves 32 KB (64 KB at D = 256) per 64 keys and workgroup, out of L2: 8
 // heads on 8 XCDs fetch 0.16 GB of K, V and Q from memory.  Two workgroups of four
 // waves share a compute unit (237 registers, 65 KB): while one waits for a tile or
 // exponentiates the other multiplies.  Short sequences pay 5-6 us per workgroup for
-// its first loads and its end (24 of up to 2300 tokens: 464 us, 840 TFLOP/s).
+// its first loads and its end (24 of up to 2300 tokens: 460-475 us, 820-840 TFLOP/s).
 #include "attn_core.h"
 #include "serving_internal.h"
 
@@ -35,9 +35,9 @@ __global__ __launch_bounds__(Stage<D>::kThreads, Stage<D>::kWavesPerSimd) void a
   __shared__ __align__(1024) uint8_t stage[2 * S::kBytes];
   __shared__ typename Wave::AreaType area;
   const uint32_t block = blockIdx.x;
-  // The last request that begins at or before this workgroup, by two loads of scalars:
-  // a search by halves waits for six in turn (24 prompts of up to 2300 tokens: 470 us
-  // against 426).
+  // The last request that begins at or before this workgroup, by two loads of scalars
+  // in turn; a search by halves waits for up to six (24 prompts of up to 2300 tokens:
+  // 467 us against 465).
   int ri = 0;
   if (a.count > 1) {
 #pragma unroll

@@ -88,7 +88,10 @@ PromptPlan plan_prompt(const skv_attn_config* c, const PromptBatch& reqs) {
   }
   // Workgroups of 128 rows, the most work per byte staged, where they fill three
   // quarters of the room or their keys will be split; otherwise of 64 or 32 rows with
-  // two waves per row tile (1000 queries of 16 x 256 on 8 KV heads: 30 us against 40).
+  // two waves per row tile.  128 against 64 rows: 1000 queries of 32 x 128 on 8 KV heads
+  // (half of the room) 24.1 us and 21.0, 6 x 250 (three quarters) 15.2 and 18.2, 2 x 900
+  // (nine tenths) 30.5 and 28.4; 1000 of 16 x 256 (half) 37.4 and 29.3, 4 x 360 (three
+  // quarters) 21.2 and 27.7.
   const bool splits = most_keys > 1024;
   if (blocks(4) * 4 < room * 3 && !(splits && most_rows >= 128)) {
     p.key_streams = 2;
@@ -96,7 +99,8 @@ PromptPlan plan_prompt(const skv_attn_config* c, const PromptBatch& reqs) {
   }
   // Parts of at least 256 keys that fill the room (100 queries of 32 x 128 over 30000
   // keys: 474 us in one part, 77 in 16); a second launch and its traffic cost about
-  // 10 us, so short keys are left whole.
+  // 10 us, so short keys are left whole.  Of at least 512: one query of 32 x 128 over
+  // 2048 keys 13.2 us against 10.5; of 128: 9.3, but 30 queries 15.0 against 14.4.
   const int64_t all = std::max<int64_t>(1, blocks(p.row_tiles));
   p.blocks = static_cast<uint64_t>(all);
   for (int32_t i = 0; i < reqs.n; ++i) {
@@ -148,7 +152,8 @@ DecodePlan plan_decode(const skv_decode_config* c) {
   // counted twice, the tails taken to be half as long as the longest), at most half:
   // more parts are more partial results to write and join (64 requests behind 16384
   // tokens of 8 x 128, 0.4 of them dropped: 45 us with all of the room at most, 38 with
-  // half, 47 with a quarter).  By its share against always half: 64 behind 2048 with
+  // half, 47 with a quarter), of 128 tokens at least (4 requests behind 512 of 8 x 128:
+  // 11.8 us, by 64 11.2, by 256 13.6; 40 behind 1024: 17.3, 24.8 and 18.5).  By its share against always half: 64 behind 2048 with
   // up to 3800 of their own, 123 us against 139; 12 behind 2048 of 8 x 256, 5 queries
   // each, with up to 1450, 34 against 47.
   if (c->prefix_len > 0) {
@@ -169,7 +174,10 @@ DecodePlan plan_decode(const skv_decode_config* c) {
   // its join reads at once (one request of 500 tokens of 8 x 128: 11.9 us against
   // 12.8; of 8192 of 4 x 128: 16.6 against 14.4); whole where that fills the room with
   // short ones (64 requests of up to 400 tokens: 14 us whole, 20 with a second launch
-  // for the parts).
+  // for the parts).  Whole up to 256 tokens (8 requests of 250 tokens of 8 x 128: 10.0
+  // us, cut 11.8; of 500: 14.0 whole, 12.7 cut).  Two parts from 2048 (64 requests of 100
+  // to 4000 tokens: 127 us, in one 141; all of 4000: 202 and 196; of 100 to 1500: 50 in
+  // two, 44 whole).
   const int64_t groups = H * p.tail_blocks, left = room - static_cast<int64_t>(p.prefix_groups);
   p.tail_least = tail <= 2048 && 2 * groups * c->num_requests * up(tail, 64) <= room ? 1 : 2;
   int64_t parts = std::max(left / groups, c->num_requests * static_cast<int64_t>(tail >= 2048 ? 2 : 1));

@@ -598,7 +598,7 @@ def attn_prompt(q: torch.Tensor, k, v, out: torch.Tensor, q_lens=None, kv_lens=N
     keys, else to q_lens; causal query i sees keys j <= i + n_keys - n_queries.
     scale defaults to 1/sqrt(d).  lse: float32 [sum(q_lens)][Hq], written when
     given.  ws: attn_prompt_workspace_size bytes, or None (no splitting of the
-    keys)."""
+    keys: few queries over many keys then take several times as long)."""
     dtype, device = q.dtype, q.get_device()
     if dtype not in _ATTN_TYPES:
         raise TypeError(f"q must be float16 or bfloat16, got {dtype}")
