@@ -563,8 +563,9 @@ skv_status skv_link(void* dst, const void* src, uint64_t bytes, void* host_stagi
  * the 16-bit type before their product with V, results rounded once.  NaN and
  * infinities follow IEEE softmax over the visible keys (but a key whose probability
  * underflows to 0 may have no effect, where IEEE's 0 times infinity is NaN: in binary16
- * one below 2^-33 of the row's largest); finite V give finite results; hidden keys' K
- * and V, whatever they hold, have no effect.
+ * one below 2^-33 of the row's largest); finite V give finite results (but where the
+ * roundings carry one past the type's largest value); hidden keys' K and V, whatever
+ * they hold, have no effect.
  * There is no soft cap of the logits and no sliding window; layers that need one cannot
  * be run by these calls.
  * Results of a call are the same every time. */
@@ -631,7 +632,9 @@ typedef struct skv_decode_config {
   int32_t table_width;   /* entries of a request's block table; times block_size
                             at most 2^30                                          */
   int32_t max_len;       /* about the longest request's tokens: sizes the launch;
-                            any request may be shorter or longer                  */
+                            any request may be shorter or longer (with more than
+                            256 requests, or one much longer than max_len, the
+                            longest one's workgroups may end last)                */
   int32_t prefix_len;    /* tokens at the start of every request that are the same
                             cache rows: a multiple of block_size whose entries in
                             every request's table are those of request 0, with the

@@ -603,7 +603,8 @@ struct WaveAttention {
   __device__ __forceinline__ void merge_state(const uint8_t* from) {
     const floatx4* f = reinterpret_cast<const floatx4*>(from) + (threadIdx.x & 63);
     const floatx2 ml = reinterpret_cast<const floatx2*>(f - (threadIdx.x & 63) + 64 * 4 * kTiles)[threadIdx.x & 63];
-    const float mn = fmaxf(m, ml.x) + 1.0f, ref = mn == -INFINITY ? 0.0f : mn;  // (halves of two finite sums add up to one)
+    // (against twice the larger reference: two finite sums then add up to one)
+    const float mn = fmaxf(m, ml.x) + 1.0f, ref = mn == -INFINITY ? 0.0f : mn;
     const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(ml.x - ref);
     m = mn;
     l = l * a + ml.y * b;
@@ -734,8 +735,8 @@ __device__ __forceinline__ float over_wave(float v, Op op) {
 // Joins the parts of a row.  WAVES waves of a workgroup share it, every WAVES-th
 // part to each; a lane has D / 64 channels (at D = 32 the upper half of a wave
 // repeats the lower).  Finite parts are added against a reference 2^kRoom times their
-// largest, so that their sum is finite too.  A wave reads the references and sums of 64 parts at once, and
-// eight parts' sums are in flight together.
+// largest, so that their sum is finite too.  A wave reads the references and sums of 64
+// parts at once, and eight parts' sums are in flight together.
 template <int D, int WAVES>
 struct JoinedRow {
   static constexpr int kPer = D >= 64 ? D / 64 : 1;

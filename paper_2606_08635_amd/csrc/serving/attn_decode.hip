@@ -16,9 +16,9 @@
 // What bounds it: reading each kept row of K and V once (4 requests of up to 32768
 // tokens of 8 x 128, a fifth dropped: 59 us for 257 MB, 4.3 TB/s with the join, and 52
 // where the same input again is partly in cache); for few tokens the latencies in turn
-// (one request of 4096 tokens of 4 x 128:
-// 13 us, of them 1.2 to find the part, 1.9 for the list, 0.8 for the first tile, 2
-// for two tiles, 1.2 for the end, 3.5 for the join, and the launches); for a prefix
+// (one request of 4096 tokens of 4 x 128: 13 us, of them 1.2 to find the part, 1.9 for
+// the list, 0.8 for the first tile, 2 for two tiles, 1.2 for the end, 3.5 for the join,
+// and the launches); for a prefix
 // under many requests its partial results (64 requests behind 16384 tokens, 0.4 of
 // them dropped: 31 us and 18 MB of sums, which the join reads in 6.5).
 #include "attn_core.h"

@@ -153,9 +153,9 @@ DecodePlan plan_decode(const skv_decode_config* c) {
   // more parts are more partial results to write and join (64 requests behind 16384
   // tokens of 8 x 128, 0.4 of them dropped: 45 us with all of the room at most, 38 with
   // half, 47 with a quarter), of 128 tokens at least (4 requests behind 512 of 8 x 128:
-  // 11.8 us, by 64 11.2, by 256 13.6; 40 behind 1024: 17.3, 24.8 and 18.5).  By its share against always half: 64 behind 2048 with
-  // up to 3800 of their own, 123 us against 139; 12 behind 2048 of 8 x 256, 5 queries
-  // each, with up to 1450, 34 against 47.
+  // 11.8 us, by 64 11.2, by 256 13.6; 40 behind 1024: 17.3, 24.8 and 18.5).  By its share
+  // against always half: 64 behind 2048 with up to 3800 of their own, 123 us against 139;
+  // 12 behind 2048 of 8 x 256, 5 queries each, with up to 1450, 34 against 47.
   if (c->prefix_len > 0) {
     p.prefix_tiles = row_tiles(all);
     p.prefix_blocks = static_cast<int32_t>(up(all, 32 * p.prefix_tiles));

@@ -1,5 +1,5 @@
 """What the attention kernels' roundings can make of a result where they are known more
-closely than attn_reference assumes, and which form a prompt call runs."""
+closely than attn_reference assumes, and calls of the kernels on host tensors."""
 import torch
 
 from attn_reference import HALF_STEP
